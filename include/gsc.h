@@ -26,6 +26,13 @@
  *                        Alg. 3; Sec. 4.4, Alg. 4); on the role-reversed
  *                        map, the transposed pooling (unpooling)
  *
+ * and, for networks that put transformer blocks between the convolutions, row
+ * operators on the same features and coordinates:
+ *
+ *   gsc_layer_norm_*     layer norm and its gradients
+ *   gsc_rotary           rotary positions with several axes
+ *   gsc_gated_ffn_*      gated feed-forward block and its gradients
+ *
  * Conventions
  *   - A coordinate row is (b, x_1, ..., x_D) of int32, batch index first;
  *     1 <= D <= 7.  Coordinates are row-major n x (1 + D); the row index is
@@ -546,6 +553,96 @@ int gsc_global_pool_fwd(int32_t mode, const float* X, int64_t n, int32_t C, cons
 /* dX (n x C, overwritten) = gradient of gsc_global_pool_fwd. */
 int gsc_global_pool_bwd(int32_t mode, const float* dY, int32_t n_batch, int32_t C, const int32_t* coords, int32_t D,
                         int64_t n, const int32_t* arg, const int32_t* cnt, float* dX, void* stream);
+
+/* ------------------------------------------------------------------------ */
+/* Row operators of transformer blocks between convolutions: layer norm,     */
+/* rotary positions at the rows' coordinates, gated feed-forward.            */
+/* float32 or bfloat16 rows (n x c, any address); sums in float32 at least.  */
+/* Results are bit-reproducible: no atomics, every sum in a fixed order.     */
+/* Arrays do not overlap except where it is said that they may be the same.  */
+/* ------------------------------------------------------------------------ */
+/* Layer norm over the channels of each row: m = mean(x), v = mean((x - m)^2),
+ * r = 1 / sqrt(v + eps), y = (x - m) r gamma + beta.  X, Y: n x c of dtype (Y
+ * may be X itself); gamma, beta: c float32 values, each nullable (null: 1 and
+ * 0); eps >= 0.  mean, rstd (n float32 values, each nullable) receive m and r,
+ * which the backward pass takes.  n = 0 does nothing.  A row with a NaN or an
+ * infinity becomes NaN, and no other row does.  Asynchronous.  Errors: EINVAL
+ * (c from 1 to 2^30), EHIP. */
+int gsc_layer_norm_fwd(int32_t dtype, const void* X, int64_t n, int32_t c, const float* gamma, const float* beta,
+                       float eps, void* Y, float* mean, float* rstd, void* stream);
+
+/* Gradients of gsc_layer_norm_fwd.  With h = (x - m) r and g = dy gamma:
+ *   dX = r (g - mean(g) - h mean(g h))   (n x c of dtype; may be X or dY itself),
+ *   dgamma = sum over rows of dy h,  dbeta = sum over rows of dy   (c float32),
+ * each nullable.  mean, rstd: as the forward pass wrote them.  With n = 0 the
+ * sums are 0.  ws: gsc_layer_norm_bwd_ws_bytes(n, c) bytes, needed only for
+ * the sums, aligned to 4 bytes.  Asynchronous.  Errors: EINVAL, ESHORT (ws),
+ * EHIP. */
+size_t gsc_layer_norm_bwd_ws_bytes(int64_t n, int32_t c);
+int gsc_layer_norm_bwd(int32_t dtype, const void* X, const void* dY, int64_t n, int32_t c, const float* gamma,
+                       const float* mean, const float* rstd, void* dX, float* dgamma, float* dbeta, void* ws,
+                       size_t ws_bytes, void* stream);
+
+/* Rotary positions: the pairs of channels of every head turned by angles that
+ * follow the row's coordinates.  X holds n rows of `heads` heads of d channels
+ * (d even, at most 4096), row i at X + i * ldx elements (ldx >= heads * d, so
+ * the queries and keys inside wider rows can be taken where they lie); Y alike
+ * with ldy (Y may be X itself, with ldy = ldx; other channels of wider rows are
+ * left alone).  coords: n x (1 + D) int32, batch index first, 1 <= D <= 7.
+ *
+ * axis_pairs (host, D ints >= 0, at most d / 2 in all) says how many pairs
+ * follow each axis: the first axis_pairs[0] pairs of a head the first axis, and
+ * so on; pairs behind the last stay as they are.  Pair j of the P pairs of axis
+ * a turns by t = x_a * axis_scale[a] * base^(-j / P):
+ *   (u, v) -> (u cos t - v sin t, u sin t + v cos t),
+ * by -t with inverse != 0 (the rotation's gradient and its undoing).  axis_scale
+ * (host, D doubles of size 1e6 at most, nullable: 1) takes coordinates to the
+ * units of the positions (a voxel size, 1 / tensor stride); base >= 1 (10000 is
+ * usual).  Pair p of a head is channels (2 p, 2 p + 1) for GSC_ROTARY_ADJACENT,
+ * (p, p + d / 2) for GSC_ROTARY_HALVES.  Angles are float64 until they are
+ * reduced to one turn.  Asynchronous.  Errors: EINVAL, EHIP. */
+typedef enum { GSC_ROTARY_ADJACENT = 0, GSC_ROTARY_HALVES = 1 } gsc_rotary_pairing;
+int gsc_rotary(int32_t dtype, const void* X, int64_t n, int32_t heads, int32_t d, int64_t ldx, const int32_t* coords,
+               int32_t D, const int32_t* axis_pairs, const double* axis_scale, double base, int32_t pairing,
+               int32_t inverse, void* Y, int64_t ldy, void* stream);
+
+/* Gated feed-forward block: Y = (act(X Wg) * (X Wu)) Wd, the product * taken
+ * element by element.  X: n x c_in, Wg and Wu: c_in x hidden, Wd: hidden x
+ * c_out, Y: n x c_out, all of dtype and row-major, widths from 1 to 2^20.  act:
+ *   SILU g / (1 + exp(-g)),  GELU g P(g) with P the normal distribution function,
+ *   GELU_TANH g (1 + tanh(sqrt(2 / pi) (g + 0.044715 g^3))) / 2,
+ *   RELU max(g, 0) (NaN passes through),  SIGMOID 1 / (1 + exp(-g)).
+ * bfloat16: products on bfloat16 operands with float32 sums; the hidden rows
+ * act(X Wg) * (X Wu) are rounded to bfloat16 once between the two products.
+ * ws: gsc_gated_ffn_fwd_ws_bytes bytes (the hidden rows), aligned to 16 bytes,
+ * contents not kept; calls that may overlap need one each.  Asynchronous.
+ * Errors: EINVAL, ESHORT (ws), EHIP. */
+typedef enum {
+    GSC_GATE_SILU = 0,
+    GSC_GATE_GELU = 1,
+    GSC_GATE_GELU_TANH = 2,
+    GSC_GATE_RELU = 3,
+    GSC_GATE_SIGMOID = 4
+} gsc_gate;
+size_t gsc_gated_ffn_fwd_ws_bytes(int32_t dtype, int64_t n, int32_t c_in, int32_t hidden, int32_t c_out);
+int gsc_gated_ffn_fwd(int32_t dtype, const void* X, int64_t n, int32_t c_in, const void* Wg, const void* Wu,
+                      int32_t hidden, const void* Wd, int32_t c_out, int32_t act, void* Y, void* ws, size_t ws_bytes,
+                      void* stream);
+
+/* Gradients of gsc_gated_ffn_fwd from its inputs (nothing of the forward pass
+ * is kept: the hidden rows are worked out again).  With G = X Wg, U = X Wu, H =
+ * act(G) * U and dH = dY Wd^T: dG = dH * U * act'(G), dU = dH * act(G),
+ *   dX = dG Wg^T + dU Wu^T (n x c_in),  dWg = X^T dG,  dWu = X^T dU,  dWd = H^T dY,
+ * each of dtype and nullable, overwritten.  (RELU: act'(0) = 0.)  bfloat16: H,
+ * dG and dU are rounded to bfloat16 once as operands of the last products, whose
+ * sums stay in float32 until the results are rounded; the weights' gradients
+ * therefore carry no more digits than bfloat16's.  With n = 0 the weights'
+ * gradients are 0.  ws: gsc_gated_ffn_bwd_ws_bytes bytes, aligned to 16 bytes,
+ * contents not kept.  Asynchronous.  Errors: EINVAL, ESHORT (ws), EHIP. */
+size_t gsc_gated_ffn_bwd_ws_bytes(int32_t dtype, int64_t n, int32_t c_in, int32_t hidden, int32_t c_out);
+int gsc_gated_ffn_bwd(int32_t dtype, const void* X, int64_t n, int32_t c_in, const void* Wg, const void* Wu,
+                      int32_t hidden, const void* Wd, int32_t c_out, const void* dY, int32_t act, void* dX, void* dWg,
+                      void* dWu, void* dWd, void* ws, size_t ws_bytes, void* stream);
 
 #ifdef __cplusplus
 }

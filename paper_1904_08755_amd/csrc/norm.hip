@@ -1,0 +1,433 @@
+// Layer norm of feature rows, forward and backward.
+//
+//   m = mean(x),  v = mean((x - m)^2),  r = 1 / sqrt(v + eps),  h = (x - m) r,  y = h gamma + beta
+//   g = dy gamma,  dx = r (g - mean(g) - h mean(g h)),  dgamma = sum over rows of dy h,  dbeta = sum of dy
+//
+// All sums are held in float32 (the sums over rows end in float64), in a fixed order: results are
+// bit-reproducible.  The mean is taken of x - x[0], so a row whose values share a large offset
+// loses no digits of its variance.
+//
+// Bound: HBM (a read and a write of n x c forward, two reads and a write backward).  A row stays
+// in the registers of LPR lanes (NV pieces of 16 bytes a lane), so it is read once; a wave holds
+// 64 / LPR rows, reduces each with log2(LPR) lane exchanges and needs no LDS, and the lanes keep
+// their columns' gamma, beta and (backward) column sums in registers over all rows they visit.
+// Rows of more than kLnRegCols columns take a block each and are read again for each sum (from the L2).
+#include "row_vec.h"
+
+namespace gsc {
+
+constexpr int kLnThreads = 256;
+constexpr int kLnRegCols = 2048;       // 32 elements a lane of a wave
+constexpr int kLnMaxCols = 1 << 30;
+constexpr int64_t kLnFwdBlocks = 2048;  // blocks that walk over the rows (8 a CU)
+constexpr int64_t kLnChunks = 1024;     // row chunks (blocks) of the backward pass: as many partial column sums
+constexpr int kLnSumCh = 16, kLnSumLanes = 64;
+
+static int64_t ln_row_blocks(int64_t n, int rows, int64_t most) {
+    const int64_t b = (n + rows - 1) / rows;
+    return b < 1 ? 1 : (b > most ? most : b);
+}
+
+template <int LPR>
+__device__ __forceinline__ float row_sum(float v) {
+#pragma unroll
+    for (int d = LPR / 2; d >= 1; d >>= 1) v += __shfl_xor(v, d, 64);
+    return v;
+}
+
+// V values of a per-column float32 array (null: the value `none`), 0 behind its end
+template <int V>
+__device__ __forceinline__ void load_cols(const float* p, int col, int c, float none, float (&v)[V]) {
+#pragma unroll
+    for (int e = 0; e < V; ++e) v[e] = col + e < c ? (p ? p[col + e] : none) : 0.f;
+}
+
+template <typename T, int LPR, int NV, bool TAIL>
+__global__ void __launch_bounds__(kLnThreads) k_ln_fwd(const T* X, int64_t n, int c, const float* __restrict__ gamma,
+                                                       const float* __restrict__ beta, float eps, T* Y,
+                                                       float* __restrict__ mean, float* __restrict__ rstd) {
+    typedef RowVec<T> R;
+    constexpr int V = R::V, RPB = kLnThreads / LPR;
+    const int l = threadIdx.x % LPR;
+    const float inv_c = 1.f / (float)c;
+    float ga[NV][V], be[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        load_cols<V>(gamma, (i * LPR + l) * V, c, 1.f, ga[i]);
+        load_cols<V>(beta, (i * LPR + l) * V, c, 0.f, be[i]);
+    }
+    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR; row < n; row += (int64_t)gridDim.x * RPB) {
+        const T* x = X + row * c;
+        typename R::Raw raw[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * LPR + l) * V;
+            raw[i] = load_vec<T, TAIL>(x + col, c - col);
+        }
+        const float x0 = __shfl(R::get(raw[0], 0), 0, LPR);   // the row's first element
+        float v[NV][V], s = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const bool in = (i * LPR + l) * V + (TAIL ? e : 0) < c;
+                v[i][e] = in ? R::get(raw[i], e) - x0 : 0.f;
+                s += v[i][e];
+            }
+        const float m = row_sum<LPR>(s) * inv_c;
+        float q = 0.f;
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const bool in = (i * LPR + l) * V + (TAIL ? e : 0) < c;
+                v[i][e] = in ? v[i][e] - m : 0.f;
+                q = fmaf(v[i][e], v[i][e], q);
+            }
+        const float r = 1.f / sqrtf(row_sum<LPR>(q) * inv_c + eps);
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * LPR + l) * V;
+            float o[V];
+#pragma unroll
+            for (int e = 0; e < V; ++e) o[e] = fmaf(v[i][e] * r, ga[i][e], be[i][e]);
+            store_vec<T, TAIL>(Y + row * c + col, c - col, o);
+        }
+        if (l == 0) {
+            if (mean) mean[row] = x0 + m;
+            if (rstd) rstd[row] = r;
+        }
+    }
+}
+
+// Sum over a block's threads (every thread gets it); sh: one float per wave.
+__device__ __forceinline__ float ln_block_sum(float v, float* sh) {
+    v = row_sum<64>(v);
+    __syncthreads();   // the previous sum is read
+    if ((threadIdx.x & 63) == 0) sh[threadIdx.x >> 6] = v;
+    __syncthreads();
+    v = 0.f;
+    for (int w = 0; w < kLnThreads / 64; ++w) v += sh[w];
+    return v;
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kLnThreads) k_ln_fwd_wide(const T* X, int64_t n, int c,
+                                                            const float* __restrict__ gamma,
+                                                            const float* __restrict__ beta, float eps, T* Y,
+                                                            float* __restrict__ mean, float* __restrict__ rstd) {
+    __shared__ float sh[kLnThreads / 64];
+    for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
+        const T* x = X + row * c;
+        const float x0 = to_f32(x[0]);
+        float s = 0.f, q = 0.f;
+        for (int i = threadIdx.x; i < c; i += kLnThreads) s += to_f32(x[i]) - x0;
+        const float m = ln_block_sum(s, sh) / (float)c;
+        for (int i = threadIdx.x; i < c; i += kLnThreads) {
+            const float d = to_f32(x[i]) - x0 - m;
+            q = fmaf(d, d, q);
+        }
+        const float r = 1.f / sqrtf(ln_block_sum(q, sh) / (float)c + eps);   // (also: every thread has read x[0])
+        for (int i = threadIdx.x; i < c; i += kLnThreads)
+            store_out(&Y[row * c + i],
+                      fmaf((to_f32(x[i]) - x0 - m) * r, gamma ? gamma[i] : 1.f, beta ? beta[i] : 0.f));
+        if (threadIdx.x == 0) {
+            if (mean) mean[row] = x0 + m;
+            if (rstd) rstd[row] = r;
+        }
+    }
+}
+
+// part: per block, the c column sums of dy h, then of dy.
+template <typename T, int LPR, int NV, bool TAIL>
+__global__ void __launch_bounds__(kLnThreads) k_ln_bwd(const T* X, const T* dY, int64_t n, int c,
+                                                       const float* __restrict__ gamma,
+                                                       const float* __restrict__ mean, const float* __restrict__ rstd,
+                                                       T* dX, float* __restrict__ part) {
+    typedef RowVec<T> R;
+    constexpr int V = R::V, RPB = kLnThreads / LPR;
+    extern __shared__ float ln_red[];   // waves x c
+    const int l = threadIdx.x % LPR;
+    const float inv_c = 1.f / (float)c;
+    float ga[NV][V], sg[NV][V], sb[NV][V];
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        load_cols<V>(gamma, (i * LPR + l) * V, c, 1.f, ga[i]);
+#pragma unroll
+        for (int e = 0; e < V; ++e) sg[i][e] = sb[i][e] = 0.f;
+    }
+    for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR; row < n; row += (int64_t)gridDim.x * RPB) {
+        const T* x = X + row * c;
+        const T* dy = dY + row * c;
+        typename R::Raw xr[NV], yr[NV];
+#pragma unroll
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * LPR + l) * V;
+            xr[i] = load_vec<T, TAIL>(x + col, c - col);
+            yr[i] = load_vec<T, TAIL>(dy + col, c - col);
+        }
+        const float m = mean[row], r = rstd[row];
+        float a = 0.f, b = 0.f;   // sums of g and of g h
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                const bool in = (i * LPR + l) * V + (TAIL ? e : 0) < c;
+                const float h = in ? (R::get(xr[i], e) - m) * r : 0.f;
+                const float d = R::get(yr[i], e), g = d * ga[i][e];
+                sg[i][e] = fmaf(d, h, sg[i][e]);
+                sb[i][e] += d;
+                a += g;
+                b = fmaf(g, h, b);
+            }
+        if (dX) {
+            a = row_sum<LPR>(a) * inv_c;
+            b = row_sum<LPR>(b) * inv_c;
+#pragma unroll
+            for (int i = 0; i < NV; ++i) {
+                const int col = (i * LPR + l) * V;
+                float o[V];
+#pragma unroll
+                for (int e = 0; e < V; ++e) {
+                    const float h = (R::get(xr[i], e) - m) * r;
+                    o[e] = r * (R::get(yr[i], e) * ga[i][e] - a - h * b);
+                }
+                store_vec<T, TAIL>(dX + row * c + col, c - col, o);
+            }
+        }
+    }
+    if (!part) return;
+    // the rows of a wave, then the waves, in a fixed order
+    const int w = threadIdx.x >> 6;
+    for (int k = 0; k < 2; ++k) {
+#pragma unroll
+        for (int i = 0; i < NV; ++i)
+#pragma unroll
+            for (int e = 0; e < V; ++e) {
+                float s = k ? sb[i][e] : sg[i][e];
+#pragma unroll
+                for (int d = LPR; d < 64; d <<= 1) s += __shfl_xor(s, d, 64);
+                const int col = (i * LPR + l) * V + e;
+                if ((threadIdx.x & 63) < LPR && col < c) ln_red[w * c + col] = s;
+            }
+        __syncthreads();
+        for (int col = threadIdx.x; col < c; col += kLnThreads) {
+            float s = 0.f;
+            for (int u = 0; u < kLnThreads / 64; ++u) s += ln_red[u * c + col];
+            part[((int64_t)blockIdx.x * 2 + k) * c + col] = s;
+        }
+        __syncthreads();
+    }
+}
+
+template <typename T>
+__global__ void __launch_bounds__(kLnThreads) k_ln_bwd_wide(const T* X, const T* dY, int64_t n, int c,
+                                                            const float* __restrict__ gamma,
+                                                            const float* __restrict__ mean,
+                                                            const float* __restrict__ rstd, T* dX) {
+    __shared__ float sh[kLnThreads / 64];
+    for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
+        const T* x = X + row * c;
+        const T* dy = dY + row * c;
+        const float m = mean[row], r = rstd[row];
+        float a = 0.f, b = 0.f;
+        for (int i = threadIdx.x; i < c; i += kLnThreads) {
+            const float g = to_f32(dy[i]) * (gamma ? gamma[i] : 1.f);
+            a += g;
+            b = fmaf(g, (to_f32(x[i]) - m) * r, b);
+        }
+        a = ln_block_sum(a, sh) / (float)c;
+        b = ln_block_sum(b, sh) / (float)c;
+        for (int i = threadIdx.x; i < c; i += kLnThreads) {
+            const float g = to_f32(dy[i]) * (gamma ? gamma[i] : 1.f), h = (to_f32(x[i]) - m) * r;
+            store_out(&dX[row * c + i], r * (g - a - h * b));
+        }
+    }
+}
+
+// Column sums of wide rows: a thread takes a column of a chunk's rows.
+template <typename T>
+__global__ void __launch_bounds__(kLnThreads) k_ln_bwd_wide_cols(const T* __restrict__ X, const T* __restrict__ dY,
+                                                                 int64_t n, int c, const float* __restrict__ mean,
+                                                                 const float* __restrict__ rstd,
+                                                                 float* __restrict__ part) {
+    const int64_t chunks = gridDim.x, k = blockIdx.x;
+    const int64_t r0 = n * k / chunks, r1 = n * (k + 1) / chunks;
+    for (int col = blockIdx.y * kLnThreads + threadIdx.x; col < c; col += gridDim.y * kLnThreads) {
+        float sg = 0.f, sb = 0.f;
+#pragma unroll 4
+        for (int64_t row = r0; row < r1; ++row) {
+            const float d = to_f32(dY[row * c + col]);
+            sg = fmaf(d, (to_f32(X[row * c + col]) - mean[row]) * rstd[row], sg);
+            sb += d;
+        }
+        part[k * 2 * c + col] = sg;
+        part[(k * 2 + 1) * c + col] = sb;
+    }
+}
+
+// The 2 c column sums from the chunks' sums: lane l of a column adds chunks l, l + 64, ... in
+// float64, then the lanes' sums pairwise.
+__global__ void __launch_bounds__(kLnSumCh * kLnSumLanes)
+k_ln_bwd_sum(const float* __restrict__ part, int64_t chunks, int c, float* __restrict__ dgamma,
+             float* __restrict__ dbeta) {
+    __shared__ double sh[kLnSumLanes][kLnSumCh];
+    const int ci = threadIdx.x % kLnSumCh, l = threadIdx.x / kLnSumCh;
+    const int64_t ch = (int64_t)blockIdx.x * kLnSumCh + ci, c2 = 2 * (int64_t)c;
+    double a = 0.0;
+    if (ch < c2) {
+#pragma unroll 4
+        for (int64_t k = l; k < chunks; k += kLnSumLanes) a += part[k * c2 + ch];
+    }
+    sh[l][ci] = a;
+    for (int d = kLnSumLanes / 2; d > 0; d >>= 1) {
+        __syncthreads();
+        if (l < d) sh[l][ci] += sh[l + d][ci];
+    }
+    if (l == 0 && ch < c2) {
+        if (ch < c) {
+            if (dgamma) dgamma[ch] = (float)sh[0][ci];
+        } else if (dbeta) {
+            dbeta[ch - c] = (float)sh[0][ci];
+        }
+    }
+}
+
+// f(LPR, NV, TAIL as constants) for rows of c <= kLnRegCols columns: the fewest lanes a row that hold
+// it in `most` pieces a lane, a whole wave with more pieces for the widest.
+template <typename T, int MOST, typename F>
+static void ln_dispatch(int c, F f) {
+    constexpr int V = RowVec<T>::V;
+    const int vecs = (c + V - 1) / V;
+    const bool tail = c % V != 0;
+    auto with = [&](auto LPR, auto NV) {
+        if (tail) f(LPR, NV, std::true_type{});
+        else f(LPR, NV, std::false_type{});
+    };
+    auto lanes = [&](auto LPR) {
+        constexpr int L = decltype(LPR)::value;
+        const int nv = (vecs + L - 1) / L;
+        if (nv <= 1) return with(LPR, std::integral_constant<int, 1>{});
+        if (MOST == 2 || nv == 2) return with(LPR, std::integral_constant<int, 2>{});
+        if constexpr (MOST > 2) {
+            if (nv == 3) return with(LPR, std::integral_constant<int, 3>{});
+            return with(LPR, std::integral_constant<int, 4>{});
+        }
+    };
+    if (vecs <= 8 * MOST) return lanes(std::integral_constant<int, 8>{});
+    if (vecs <= 16 * MOST) return lanes(std::integral_constant<int, 16>{});
+    if (vecs <= 32 * MOST) return lanes(std::integral_constant<int, 32>{});
+    if (vecs <= 64 * MOST) return lanes(std::integral_constant<int, 64>{});
+    constexpr std::integral_constant<int, 64> W{};
+    if (MOST == 2 && vecs <= 64 * 3) return with(W, std::integral_constant<int, 3>{});
+    if (MOST == 2 && vecs <= 64 * 4) return with(W, std::integral_constant<int, 4>{});
+    if constexpr (V == 4) {   // float32 rows: up to 512 pieces
+        if (vecs <= 64 * 6) return with(W, std::integral_constant<int, 6>{});
+        return with(W, std::integral_constant<int, 8>{});
+    }
+}
+
+template <typename T>
+static void ln_fwd(const void* X_, int64_t n, int c, const float* gamma, const float* beta, float eps, void* Y_,
+                   float* mean, float* rstd, hipStream_t s) {
+    const T* X = reinterpret_cast<const T*>(X_);
+    T* Y = reinterpret_cast<T*>(Y_);
+    if (c > kLnRegCols) {
+        hipLaunchKernelGGL(k_ln_fwd_wide<T>, dim3((unsigned)ln_row_blocks(n, 1, kLnFwdBlocks)), dim3(kLnThreads), 0, s,
+                           X, n, c, gamma, beta, eps, Y, mean, rstd);
+        return;
+    }
+    ln_dispatch<T, 4>(c, [&](auto LPR, auto NV, auto TAIL) {
+        constexpr int L = decltype(LPR)::value, N = decltype(NV)::value;
+        auto* kern = k_ln_fwd<T, L, N, decltype(TAIL)::value>;
+        hipLaunchKernelGGL(kern, dim3((unsigned)ln_row_blocks(n, kLnThreads / L, kLnFwdBlocks)), dim3(kLnThreads), 0, s,
+                           X, n, c, gamma, beta, eps, Y, mean, rstd);
+    });
+}
+
+// Launches the passes over the rows; returns the number of chunks whose sums are in part.
+template <typename T>
+static int64_t ln_bwd(const void* X_, const void* dY_, int64_t n, int c, const float* gamma, const float* mean,
+                      const float* rstd, void* dX_, float* part, hipStream_t s) {
+    const T* X = reinterpret_cast<const T*>(X_);
+    const T* dY = reinterpret_cast<const T*>(dY_);
+    T* dX = reinterpret_cast<T*>(dX_);
+    int64_t chunks = 0;
+    if (c > kLnRegCols) {
+        chunks = ln_row_blocks(n, 64, kLnChunks);
+        const unsigned cb = (unsigned)((c + kLnThreads - 1) / kLnThreads);
+        if (part)   // before dX is written, which may be dY itself
+            hipLaunchKernelGGL(k_ln_bwd_wide_cols<T>, dim3((unsigned)chunks, cb < 4096 ? cb : 4096), dim3(kLnThreads),
+                               0, s, X, dY, n, c, mean, rstd, part);
+        if (dX && n > 0)
+            hipLaunchKernelGGL(k_ln_bwd_wide<T>, dim3((unsigned)ln_row_blocks(n, 1, kLnFwdBlocks)), dim3(kLnThreads),
+                               0, s, X, dY, n, c, gamma, mean, rstd, dX);
+        return chunks;
+    }
+    ln_dispatch<T, 2>(c, [&](auto LPR, auto NV, auto TAIL) {
+        constexpr int L = decltype(LPR)::value, N = decltype(NV)::value;
+        auto* kern = k_ln_bwd<T, L, N, decltype(TAIL)::value>;
+        chunks = ln_row_blocks(n, kLnThreads / L, kLnChunks);
+        hipLaunchKernelGGL(kern, dim3((unsigned)chunks), dim3(kLnThreads),
+                           part ? (kLnThreads / 64) * c * sizeof(float) : 0, s, X, dY, n, c, gamma, mean, rstd, dX,
+                           part);
+    });
+    return chunks;
+}
+
+}  // namespace gsc
+
+using namespace gsc;
+
+extern "C" {
+
+int gsc_layer_norm_fwd(int32_t dtype, const void* X, int64_t n, int32_t c, const float* gamma, const float* beta,
+                       float eps, void* Y, float* mean, float* rstd, void* stream) {
+    clear_error();
+    if (dtype != GSC_F32 && dtype != GSC_BF16) return fail(GSC_EINVAL, "layer_norm_fwd: unknown dtype %d", dtype);
+    if (n < 0 || c < 1 || c > kLnMaxCols) return fail(GSC_EINVAL, "layer_norm_fwd: bad sizes n=%lld c=%d", (long long)n, c);
+    if (!(eps >= 0.f) || eps > 3.4e38f) return fail(GSC_EINVAL, "layer_norm_fwd: eps must be finite and not negative");
+    if (n == 0) return GSC_OK;
+    if (!X || !Y) return fail(GSC_EINVAL, "layer_norm_fwd: null X/Y");
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    if (dtype == GSC_BF16) ln_fwd<uint16_t>(X, n, c, gamma, beta, eps, Y, mean, rstd, s);
+    else ln_fwd<float>(X, n, c, gamma, beta, eps, Y, mean, rstd, s);
+    GSC_LAUNCH_CHECK();
+    return GSC_OK;
+}
+
+size_t gsc_layer_norm_bwd_ws_bytes(int64_t n, int32_t c) {
+    if (n < 0 || c < 1 || c > kLnMaxCols) return 0;
+    return (size_t)ln_row_blocks(n, kLnThreads / 64, kLnChunks) * 2 * (size_t)c * sizeof(float);
+}
+
+int gsc_layer_norm_bwd(int32_t dtype, const void* X, const void* dY, int64_t n, int32_t c, const float* gamma,
+                       const float* mean, const float* rstd, void* dX, float* dgamma, float* dbeta, void* ws,
+                       size_t ws_bytes, void* stream) {
+    clear_error();
+    if (dtype != GSC_F32 && dtype != GSC_BF16) return fail(GSC_EINVAL, "layer_norm_bwd: unknown dtype %d", dtype);
+    if (n < 0 || c < 1 || c > kLnMaxCols) return fail(GSC_EINVAL, "layer_norm_bwd: bad sizes n=%lld c=%d", (long long)n, c);
+    if (n > 0 && (!X || !dY || !mean || !rstd)) return fail(GSC_EINVAL, "layer_norm_bwd: null X/dY/mean/rstd");
+    const bool sums = dgamma || dbeta;
+    if (sums) {
+        const size_t need = gsc_layer_norm_bwd_ws_bytes(n, c);
+        if (!ws || ws_bytes < need)
+            return fail(GSC_ESHORT, "layer_norm_bwd: ws needs %zu bytes, got %zu", need, ws ? ws_bytes : (size_t)0);
+        if (reinterpret_cast<uintptr_t>(ws) % alignof(float))
+            return fail(GSC_EINVAL, "layer_norm_bwd: ws must be aligned to 4 bytes");
+    }
+    if (!sums && (!dX || n == 0)) return GSC_OK;
+    hipStream_t s = reinterpret_cast<hipStream_t>(stream);
+    float* part = sums ? reinterpret_cast<float*>(ws) : nullptr;
+    const int64_t chunks = dtype == GSC_BF16 ? ln_bwd<uint16_t>(X, dY, n, c, gamma, mean, rstd, dX, part, s)
+                                             : ln_bwd<float>(X, dY, n, c, gamma, mean, rstd, dX, part, s);
+    GSC_LAUNCH_CHECK();
+    if (sums) {
+        hipLaunchKernelGGL(k_ln_bwd_sum, dim3((unsigned)((2 * (int64_t)c + kLnSumCh - 1) / kLnSumCh)),
+                           dim3(kLnSumCh * kLnSumLanes), 0, s, part, chunks, c, dgamma, dbeta);
+        GSC_LAUNCH_CHECK();
+    }
+    return GSC_OK;
+}
+
+}  // extern "C"

@@ -1,0 +1,78 @@
+// Rows of features as 16-byte pieces, for the row-wise operators (norm.hip, rotary.hip).
+#pragma once
+
+#include "conv_common.h"
+
+namespace gsc {
+
+typedef __bf16 rv_bf16x2 __attribute__((ext_vector_type(2)));
+typedef float rv_floatx2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector(rv_floatx2{lo, hi}, rv_bf16x2));
+}
+
+// 16 bytes of a row that may start at any element: one load or store, without the promise of a
+// 16-byte address to the compiler.
+template <typename T>
+struct RowVec;
+template <>
+struct RowVec<float> {
+    static constexpr int V = 4;
+    typedef uint32_t Raw __attribute__((ext_vector_type(4), aligned(4)));
+    static __device__ __forceinline__ float get(const Raw& r, int e) { return __uint_as_float(r[e]); }
+    static __device__ __forceinline__ Raw put(const float (&v)[V]) {
+        Raw r;
+#pragma unroll
+        for (int e = 0; e < V; ++e) r[e] = __float_as_uint(v[e]);
+        return r;
+    }
+};
+template <>
+struct RowVec<uint16_t> {
+    static constexpr int V = 8;
+    typedef uint32_t Raw __attribute__((ext_vector_type(4), aligned(2)));
+    static __device__ __forceinline__ float get(const Raw& r, int e) {
+        return __uint_as_float(e & 1 ? r[e >> 1] & 0xffff0000u : r[e >> 1] << 16);
+    }
+    static __device__ __forceinline__ Raw put(const float (&v)[V]) {
+        Raw r;
+#pragma unroll
+        for (int e = 0; e < V / 2; ++e) r[e] = pack_bf16(v[2 * e], v[2 * e + 1]);
+        return r;
+    }
+};
+
+// Elements [0, left) of 16 bytes, zeros behind them.  TAIL = false: left is 0 or at least V.
+template <typename T, bool TAIL>
+__device__ __forceinline__ typename RowVec<T>::Raw load_vec(const T* p, int64_t left) {
+    typedef RowVec<T> R;
+    typename R::Raw r = {0, 0, 0, 0};
+    if (left >= R::V) {
+        r = *reinterpret_cast<const typename R::Raw*>(p);
+    } else if (TAIL && left > 0) {
+        if constexpr (sizeof(T) == 4) {
+            for (int e = 0; e < R::V; ++e)
+                if (e < left) r[e] = __float_as_uint(p[e]);
+        } else {
+#pragma unroll
+            for (int e = 0; e < R::V; ++e)
+                if (e < left) r[e >> 1] |= (uint32_t)p[e] << (16 * (e & 1));
+        }
+    }
+    return r;
+}
+
+template <typename T, bool TAIL>
+__device__ __forceinline__ void store_vec(T* p, int64_t left, const float (&v)[RowVec<T>::V]) {
+    typedef RowVec<T> R;
+    if (left >= R::V) {
+        *reinterpret_cast<typename R::Raw*>(p) = R::put(v);
+    } else if (TAIL) {
+#pragma unroll
+        for (int e = 0; e < R::V; ++e)
+            if (e < left) store_out(&p[e], v[e]);
+    }
+}
+
+}  // namespace gsc

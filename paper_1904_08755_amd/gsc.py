@@ -8,6 +8,7 @@ library is missing, loading fails with an error (there is no fallback).
 """
 from __future__ import annotations
 
+import contextlib
 import ctypes
 import dataclasses
 import os
@@ -88,6 +89,16 @@ _SIGS = {
     "gsc_global_pool_ws_bytes": (_sz, [_i64, _i32, _i32]),
     "gsc_global_pool_fwd": (ctypes.c_int, [_i32, _vp, _i64, _i32, _vp, _i32, _i32, _vp, _vp, _vp, _vp, _sz, _vp]),
     "gsc_global_pool_bwd": (ctypes.c_int, [_i32, _vp, _i32, _i32, _vp, _i32, _i64, _vp, _vp, _vp, _vp]),
+    "gsc_layer_norm_fwd": (ctypes.c_int, [_i32, _vp, _i64, _i32, _vp, _vp, ctypes.c_float, _vp, _vp, _vp, _vp]),
+    "gsc_layer_norm_bwd_ws_bytes": (_sz, [_i64, _i32]),
+    "gsc_layer_norm_bwd": (ctypes.c_int, [_i32, _vp, _vp, _i64, _i32, _vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _vp]),
+    "gsc_rotary": (ctypes.c_int, [_i32, _vp, _i64, _i32, _i32, _i64, _vp, _i32, _c_i32p,
+                                  ctypes.POINTER(ctypes.c_double), ctypes.c_double, _i32, _i32, _vp, _i64, _vp]),
+    "gsc_gated_ffn_fwd_ws_bytes": (_sz, [_i32, _i64, _i32, _i32, _i32]),
+    "gsc_gated_ffn_fwd": (ctypes.c_int, [_i32, _vp, _i64, _i32, _vp, _vp, _i32, _vp, _i32, _i32, _vp, _vp, _sz, _vp]),
+    "gsc_gated_ffn_bwd_ws_bytes": (_sz, [_i32, _i64, _i32, _i32, _i32]),
+    "gsc_gated_ffn_bwd": (ctypes.c_int, [_i32, _vp, _i64, _i32, _vp, _vp, _i32, _vp, _i32, _vp, _i32, _vp, _vp, _vp,
+                                         _vp, _vp, _sz, _vp]),
 }
 
 GSC_POOL_MAX, GSC_POOL_AVG, GSC_POOL_SUM = 0, 1, 2
@@ -704,3 +715,192 @@ def gsc_quantize(points: torch.Tensor, voxel, batch: Optional[torch.Tensor] = No
                               table.numel(), _ptr(ws), ws.numel(), _stream(stream)))
     m = n_out.value
     return Quantized(out[:m], rep[:m], None if out_labels is None else out_labels[:m], inverse[:n], table)
+
+
+# --------------------------------------------------------------------------- #
+# row operators of transformer blocks between convolutions
+# --------------------------------------------------------------------------- #
+GSC_ROTARY_ADJACENT, GSC_ROTARY_HALVES = 0, 1
+ROTARY_PAIRINGS = {"adjacent": GSC_ROTARY_ADJACENT, "halves": GSC_ROTARY_HALVES}
+GSC_GATE_SILU, GSC_GATE_GELU, GSC_GATE_GELU_TANH, GSC_GATE_RELU, GSC_GATE_SIGMOID = 0, 1, 2, 3, 4
+GATES = {"silu": GSC_GATE_SILU, "gelu": GSC_GATE_GELU, "gelu_tanh": GSC_GATE_GELU_TANH, "relu": GSC_GATE_RELU,
+         "sigmoid": GSC_GATE_SIGMOID}
+
+
+def _fresh(stream):
+    """Context in which the buffers of a call on ``stream`` are allocated: they belong to that stream, so neither
+    their reuse nor their earlier owners run beside it."""
+    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+
+
+def _here(X: torch.Tensor, **others):
+    """All tensors of a call (None: not given) lie on X's device, which is the current one (the stream's)."""
+    if X.device.index != torch.cuda.current_device():
+        raise ValueError(f"X is on {X.device}, the current device is cuda:{torch.cuda.current_device()}")
+    for name, t in others.items():
+        if t is not None and t.device != X.device:
+            raise ValueError(f"{name} must be on {X.device}, got {t.device}")
+
+
+def _choice(table, key, name):
+    if key not in table:
+        raise ValueError(f"{name} must be one of {sorted(table)}, got {key!r}")
+    return table[key]
+
+
+def _like(t, ref, dtype, name, dims=2):
+    _need(t, dtype, name, dims)
+    if tuple(t.shape) != tuple(ref):
+        raise ValueError(f"{name} must have shape {tuple(ref)}, got {tuple(t.shape)}")
+
+
+def gsc_layer_norm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
+                       eps: float = 1e-5, stats: bool = True, Y: Optional[torch.Tensor] = None, stream=None):
+    """Layer norm over the channels of each row: (Y, mean, rstd), the statistics float32 per row (None without
+    ``stats``; the backward pass takes them).  ``gamma`` and ``beta``: float32 per channel, each optional."""
+    dt = _dt(X)
+    _need(X, X.dtype, "X", 2)
+    n, c = X.shape
+    for name, v in (("gamma", gamma), ("beta", beta)):
+        if v is not None:
+            _like(v, (c,), torch.float32, name, 1)
+    if Y is not None:
+        _like(Y, X.shape, X.dtype, "Y")
+    _here(X, gamma=gamma, beta=beta, Y=Y)
+    with _fresh(stream):
+        if Y is None:
+            Y = torch.empty_like(X)
+        st = torch.empty((2, n), dtype=torch.float32, device=X.device) if stats else (None, None)
+    _check(lib().gsc_layer_norm_fwd(dt, _ptr(X), n, c, _ptr(gamma), _ptr(beta), eps, _ptr(Y), _ptr(st[0]), _ptr(st[1]),
+                                    _stream(stream)))
+    return Y, st[0], st[1]
+
+
+def gsc_layer_norm_bwd(X: torch.Tensor, dY: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
+                       gamma: Optional[torch.Tensor] = None, need_dx: bool = True, need_sums: bool = True,
+                       dX: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of gsc_layer_norm_fwd: (dX or None, dgamma, dbeta), the last two float32 per channel (None without
+    ``need_sums``)."""
+    dt = _dt(X)
+    _need(X, X.dtype, "X", 2)
+    n, c = X.shape
+    _like(dY, X.shape, X.dtype, "dY")
+    _like(mean, (n,), torch.float32, "mean", 1)
+    _like(rstd, (n,), torch.float32, "rstd", 1)
+    if gamma is not None:
+        _like(gamma, (c,), torch.float32, "gamma", 1)
+    if dX is not None:
+        _like(dX, X.shape, X.dtype, "dX")
+    if ws is not None:
+        _need(ws, torch.uint8, "ws", 1)
+    _here(X, dY=dY, mean=mean, rstd=rstd, gamma=gamma, dX=dX, ws=ws)
+    with _fresh(stream):
+        if need_dx and dX is None:
+            dX = torch.empty_like(X)
+        sums = torch.empty((2, c), dtype=torch.float32, device=X.device) if need_sums else (None, None)
+        if need_sums and ws is None:
+            ws = _ws(lib().gsc_layer_norm_bwd_ws_bytes(n, c), X.device)
+    _check(lib().gsc_layer_norm_bwd(dt, _ptr(X), _ptr(dY), n, c, _ptr(gamma), _ptr(mean), _ptr(rstd),
+                                    _ptr(dX) if need_dx else None, _ptr(sums[0]), _ptr(sums[1]),
+                                    _ptr(ws) if need_sums else None, ws.numel() if need_sums else 0, _stream(stream)))
+    return (dX if need_dx else None), sums[0], sums[1]
+
+
+def _heads(t: torch.Tensor, name: str) -> int:
+    """Row stride of n x heads x d rows whose heads lie next to each other."""
+    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+        raise ValueError(f"{name} must be a CUDA (HIP) tensor")
+    if t.dim() != 3:
+        raise ValueError(f"{name} must have 3 dims (rows, heads, channels)")
+    n, H, d = t.shape
+    if (d > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != d):
+        raise ValueError(f"{name}'s heads must lie next to each other in a row")
+    if n > 1 and t.stride(0) < H * d:
+        raise ValueError(f"{name}'s rows overlap")
+    return t.stride(0) if n > 1 else H * d
+
+
+def gsc_rotary(X: torch.Tensor, coords: torch.Tensor, axis_pairs: Sequence[int],
+               scale: Optional[Sequence[float]] = None, base: float = 10000.0, pairing: str = "adjacent",
+               inverse: bool = False, Y: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """The heads of ``X`` (n x heads x d; a view into wider rows is taken as it lies) turned by angles that follow
+    ``coords`` (n x (1 + D) int32): ``axis_pairs[a]`` pairs of each head by axis a, coordinates times ``scale[a]``.
+    ``inverse`` turns back (the gradient).  ``Y`` may be ``X``."""
+    dt = _dt(X)
+    ldx = _heads(X, "X")
+    _need(coords, torch.int32, "coords", 2)
+    n, H, d = X.shape
+    D = coords.shape[1] - 1
+    if coords.shape[0] != n:
+        raise ValueError(f"coords has {coords.shape[0]} rows, X {n}")
+    if len(axis_pairs) != D or (scale is not None and len(scale) != D):
+        raise ValueError(f"axis_pairs and scale need {D} entries")
+    if Y is not None and (Y.shape != X.shape or Y.dtype != X.dtype):
+        raise ValueError("Y must have X's shape and dtype")
+    _here(X, coords=coords, Y=Y)
+    pm = _choice(ROTARY_PAIRINGS, pairing, "pairing")
+    if Y is None:
+        with _fresh(stream):
+            Y = torch.empty((n, H, d), dtype=X.dtype, device=X.device)
+    ldy = _heads(Y, "Y")
+    sc = None if scale is None else (ctypes.c_double * max(D, 1))(*[float(v) for v in scale])
+    _check(lib().gsc_rotary(dt, _ptr(X), n, H, d, ldx, _ptr(coords), D,
+                            (ctypes.c_int32 * max(D, 1))(*[int(v) for v in axis_pairs]), sc, float(base), pm,
+                            1 if inverse else 0, _ptr(Y), ldy, _stream(stream)))
+    return Y
+
+
+def _ffn_args(X, Wg, Wu, Wd, act):
+    dt = _dt(X)
+    _need(X, X.dtype, "X", 2)
+    n, ci = X.shape
+    _need(Wg, X.dtype, "Wg", 2)
+    f = Wg.shape[1]
+    _like(Wg, (ci, f), X.dtype, "Wg")
+    _like(Wu, (ci, f), X.dtype, "Wu")
+    _need(Wd, X.dtype, "Wd", 2)
+    _like(Wd, (f, Wd.shape[1]), X.dtype, "Wd")
+    return dt, n, ci, f, Wd.shape[1], _choice(GATES, act, "act")
+
+
+def gsc_gated_ffn_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, act: str = "silu",
+                      Y: Optional[torch.Tensor] = None, ws: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
+    """(act(X Wg) * (X Wu)) Wd for weights c_in x hidden, c_in x hidden, hidden x c_out of X's dtype."""
+    dt, n, ci, f, co, gate = _ffn_args(X, Wg, Wu, Wd, act)
+    if Y is not None:
+        _like(Y, (n, co), X.dtype, "Y")
+    if ws is not None:
+        _need(ws, torch.uint8, "ws", 1)
+    _here(X, Wg=Wg, Wu=Wu, Wd=Wd, Y=Y, ws=ws)
+    with _fresh(stream):
+        if Y is None:
+            Y = torch.empty((n, co), dtype=X.dtype, device=X.device)
+        if ws is None:
+            ws = _ws(lib().gsc_gated_ffn_fwd_ws_bytes(dt, n, ci, f, co), X.device)
+    _check(lib().gsc_gated_ffn_fwd(dt, _ptr(X), n, ci, _ptr(Wg), _ptr(Wu), f, _ptr(Wd), co, gate, _ptr(Y), _ptr(ws),
+                                   ws.numel(), _stream(stream)))
+    return Y
+
+
+def gsc_gated_ffn_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, dY: torch.Tensor,
+                      act: str = "silu", need_dx: bool = True, need_dw: bool = True, dX: Optional[torch.Tensor] = None,
+                      ws: Optional[torch.Tensor] = None, stream=None):
+    """Gradients of gsc_gated_ffn_fwd from its inputs: (dX or None, dWg, dWu, dWd), all of X's dtype (the weights'
+    None without ``need_dw``)."""
+    dt, n, ci, f, co, gate = _ffn_args(X, Wg, Wu, Wd, act)
+    _like(dY, (n, co), X.dtype, "dY")
+    if dX is not None:
+        _like(dX, X.shape, X.dtype, "dX")
+    if ws is not None:
+        _need(ws, torch.uint8, "ws", 1)
+    _here(X, Wg=Wg, Wu=Wu, Wd=Wd, dY=dY, dX=dX, ws=ws)
+    with _fresh(stream):
+        if need_dx and dX is None:
+            dX = torch.empty_like(X)
+        dW = [torch.empty_like(W) if need_dw else None for W in (Wg, Wu, Wd)]
+        if ws is None:
+            ws = _ws(lib().gsc_gated_ffn_bwd_ws_bytes(dt, n, ci, f, co), X.device)
+    _check(lib().gsc_gated_ffn_bwd(dt, _ptr(X), n, ci, _ptr(Wg), _ptr(Wu), f, _ptr(Wd), co, _ptr(dY), gate,
+                                   _ptr(dX) if need_dx else None, *[_ptr(W) for W in dW], _ptr(ws), ws.numel(),
+                                   _stream(stream)))
+    return (dX if need_dx else None), *dW

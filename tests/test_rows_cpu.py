@@ -1,0 +1,113 @@
+"""CPU checks of the row operators (layer norm, rotary positions, gated feed-forward): host-side validation rejects
+bad arguments before any HIP call, and the workspace sizes cover what the calls write."""
+import ctypes
+import math
+import os
+
+import pytest
+import torch
+
+from paper_1904_08755_amd import gsc
+
+FAKE = ctypes.c_void_p(0x1000)   # never dereferenced: validation fails first
+
+
+@pytest.fixture(scope="module")
+def L():
+    if not os.path.exists(gsc.LIB_PATH):
+        pytest.skip("libgsc.so not built")
+    return gsc.lib()
+
+
+def _err(L):
+    return L.gsc_last_error().decode()
+
+
+def test_layer_norm_validation(L):
+    fwd = lambda dt=0, n=10, c=8, X=FAKE, Y=FAKE, eps=1e-5: L.gsc_layer_norm_fwd(dt, X, n, c, None, None, eps, Y, None,
+                                                                                None, None)
+    assert fwd(dt=2) == gsc.GSC_EINVAL and "dtype" in _err(L)
+    assert fwd(n=-1) == gsc.GSC_EINVAL
+    assert fwd(c=0) == gsc.GSC_EINVAL and "c=0" in _err(L)
+    assert fwd(c=(1 << 30) + 1) == gsc.GSC_EINVAL
+    assert fwd(X=None) == gsc.GSC_EINVAL
+    assert fwd(Y=None) == gsc.GSC_EINVAL
+    for eps in (-1e-5, math.nan, math.inf):
+        assert fwd(eps=eps) == gsc.GSC_EINVAL and "eps" in _err(L)
+    assert fwd(n=0, X=None, Y=None) == gsc.GSC_OK   # no rows: nothing is read or launched
+    need = L.gsc_layer_norm_bwd_ws_bytes(1000, 32)
+    assert need >= 250 * 2 * 32 * 4 and L.gsc_layer_norm_bwd_ws_bytes(0, 32) == 2 * 32 * 4
+    assert L.gsc_layer_norm_bwd_ws_bytes(-1, 32) == 0 and L.gsc_layer_norm_bwd_ws_bytes(5, 0) == 0
+    assert L.gsc_layer_norm_bwd_ws_bytes(10**9, 32) == 1024 * 2 * 32 * 4
+    bwd = lambda dt=0, n=1000, c=32, mean=FAKE, dX=FAKE, dg=FAKE, ws=FAKE, wsb=need: L.gsc_layer_norm_bwd(
+        dt, FAKE, FAKE, n, c, None, mean, FAKE, dX, dg, None, ws, wsb, None)
+    assert bwd(dt=-1) == gsc.GSC_EINVAL
+    assert bwd(c=0) == gsc.GSC_EINVAL
+    assert bwd(mean=None) == gsc.GSC_EINVAL
+    assert bwd(ws=None) == gsc.GSC_ESHORT and str(need) in _err(L)
+    assert bwd(wsb=need - 1) == gsc.GSC_ESHORT
+    assert bwd(ws=ctypes.c_void_p(0x1002)) == gsc.GSC_EINVAL and "aligned" in _err(L)
+    assert bwd(dX=None, dg=None, ws=None, wsb=0) == gsc.GSC_OK     # nothing asked for
+    assert bwd(n=0, dg=None, ws=None, wsb=0) == gsc.GSC_OK
+
+
+def test_rotary_validation(L):
+    def rot(dt=0, X=FAKE, n=10, heads=2, d=8, ldx=16, coords=FAKE, D=3, pairs=(1, 1, 1), scale=None, base=1e4, pairing=0,
+            Y=FAKE, ldy=16):
+        pa = None if pairs is None else (ctypes.c_int32 * 8)(*pairs)
+        sc = None if scale is None else (ctypes.c_double * 8)(*scale)
+        return L.gsc_rotary(dt, X, n, heads, d, ldx, coords, D, pa, sc, base, pairing, 0, Y, ldy, None)
+
+    for bad in (dict(dt=5), dict(n=-1), dict(heads=0), dict(d=7), dict(d=0), dict(d=4098, ldx=1 << 20, ldy=1 << 20),
+                dict(ldx=15), dict(ldy=15), dict(D=0), dict(D=8, pairs=[0] * 8), dict(pairs=None), dict(pairs=(2, 2, 1)),
+                dict(pairs=(1, -1, 1)), dict(pairs=(2**30, 2**30, 2**31 - 1)), dict(scale=(1, math.nan, 1)),
+                dict(scale=(1, 1, 2e6)), dict(base=0.5), dict(base=math.inf), dict(base=math.nan), dict(pairing=2),
+                dict(X=None), dict(Y=None), dict(coords=None), dict(ldy=17),
+                dict(heads=1 << 20, d=1 << 10, ldx=1 << 40, ldy=1 << 40)):
+        assert rot(**bad) == gsc.GSC_EINVAL, bad
+        assert "rotary" in _err(L), bad
+    assert rot(n=0, X=None, Y=None, coords=None) == gsc.GSC_OK
+
+
+def test_gated_ffn_validation(L):
+    need = L.gsc_gated_ffn_fwd_ws_bytes(gsc.GSC_BF16, 100, 64, 267, 64)
+    assert need >= 100 * 272 * 2   # hidden rows padded to whole 16-byte pieces
+    assert L.gsc_gated_ffn_fwd_ws_bytes(gsc.GSC_F32, 100, 64, 256, 64) >= 100 * 256 * 4
+    for bad in ((7, 100, 64, 64, 64), (0, -1, 64, 64, 64), (0, 1, 0, 64, 64), (0, 1, 64, 0, 64), (0, 1, 64, 64, 0),
+                (0, 1, (1 << 20) + 1, 64, 64)):
+        assert L.gsc_gated_ffn_fwd_ws_bytes(*bad) == 0 and L.gsc_gated_ffn_bwd_ws_bytes(*bad) == 0
+    fwd = lambda dt=1, X=FAKE, n=100, ci=64, f=267, co=64, act=0, Y=FAKE, ws=FAKE, wsb=need: L.gsc_gated_ffn_fwd(
+        dt, X, n, ci, FAKE, FAKE, f, FAKE, co, act, Y, ws, wsb, None)
+    for bad in (dict(dt=3), dict(X=None), dict(n=-1), dict(ci=0), dict(f=0), dict(co=0), dict(act=5), dict(act=-1),
+                dict(Y=None), dict(f=1 << 21), dict(n=1 << 34, f=1 << 20), dict(n=1 << 40)):
+        assert fwd(**bad) == gsc.GSC_EINVAL, bad
+        assert "gated_ffn_fwd" in _err(L)
+    assert fwd(ws=None) == gsc.GSC_ESHORT and fwd(wsb=need - 1) == gsc.GSC_ESHORT and str(need) in _err(L)
+    assert fwd(ws=ctypes.c_void_p(0x1008)) == gsc.GSC_EINVAL and "aligned" in _err(L)
+    assert fwd(n=0, X=None, ws=None, wsb=0) == gsc.GSC_OK
+    nb = L.gsc_gated_ffn_bwd_ws_bytes(gsc.GSC_BF16, 100, 64, 267, 64)
+    assert nb >= 3 * 100 * 272 * 2 + (64 * 2 * 272 + 267 * 64) * 4
+    assert L.gsc_gated_ffn_bwd_ws_bytes(gsc.GSC_F32, 0, 64, 256, 64) > 0
+    bwd = lambda dt=1, X=FAKE, n=100, f=267, act=0, dX=FAKE, dW=FAKE, ws=FAKE, wsb=nb: L.gsc_gated_ffn_bwd(
+        dt, X, n, 64, FAKE, FAKE, f, FAKE, 64, FAKE, act, dX, dW, dW, dW, ws, wsb, None)
+    for bad in (dict(dt=3), dict(X=None), dict(n=-1), dict(f=0), dict(act=5), dict(n=1 << 34, f=1 << 20)):
+        assert bwd(**bad) == gsc.GSC_EINVAL, bad
+        assert "gated_ffn_bwd" in _err(L)
+    assert bwd(ws=None) == gsc.GSC_ESHORT and bwd(wsb=nb - 1) == gsc.GSC_ESHORT and str(nb) in _err(L)
+    assert bwd(ws=ctypes.c_void_p(0x1008)) == gsc.GSC_EINVAL
+    assert bwd(dX=None, dW=None, ws=None, wsb=0) == gsc.GSC_OK
+    assert bwd(n=0, dW=None, ws=None, wsb=0) == gsc.GSC_OK
+
+
+def test_binding_refuses_host_tensors():
+    x = torch.zeros(4, 8)
+    with pytest.raises(ValueError, match="CUDA"):
+        gsc.gsc_layer_norm_fwd(x)
+    with pytest.raises(ValueError, match="CUDA"):
+        gsc.gsc_layer_norm_bwd(x, x, x[:, 0], x[:, 0])
+    with pytest.raises(ValueError, match="CUDA"):
+        gsc.gsc_rotary(x.view(4, 1, 8), torch.zeros(4, 4, dtype=torch.int32), [1, 1, 1])
+    with pytest.raises(ValueError, match="CUDA"):
+        gsc.gsc_gated_ffn_fwd(x, torch.zeros(8, 4), torch.zeros(8, 4), torch.zeros(4, 8))
+    with pytest.raises(ValueError, match="dtype"):
+        gsc.gsc_layer_norm_fwd(x.half())
