@@ -14,28 +14,18 @@
 // k_ffn_dw_sum adds the chunks in order, so that every result is bit-reproducible.
 //
 // bfloat16: G, U, dH and all sums stay in float32; H, dG and dU are rounded to bfloat16 once, as the
-// matrix cores take them, and the results once as they are stored.
-//
-// One tile product serves all of them (tile_product): 32 MT x 32 NT outputs per block of four waves,
-// the operands' next 128 bytes of the reduction in registers while the current ones are read from
-// LDS (two stages, one barrier a step).  An operand lies either with the reduction along its rows
-// (KC) or across them (MC); both are copied to LDS as they lie, and an MC operand's bfloat16 fragments
-// are read with the LDS transpose read (ds_read_b64_tr_b16: within each 16 lanes, lane i receives
-// element i % 4 of the 8-byte pieces that lanes i / 4, i / 4 + 4, i / 4 + 8, i / 4 + 12 address).
-#include "row_vec.h"
+// matrix cores take them, and the results once as they are stored.  Its tiles copy operands straight
+// into LDS (ffn_bf16.h), which takes rows of whole 16-byte pieces at 16-byte addresses: operands that are not
+// are copied into the workspace first, their rows padded with zeros (k_ffn_pad; the weights and at
+// most three passes over rows, against kernels that would load element by element).  float32 tiles
+// (ffn_f32.h) take any address.
+#include "ffn_bf16.h"
+#include "ffn_f32.h"
 
 namespace gsc {
 
-constexpr int kFfnThreads = 256;
-constexpr int kFfnRowBytes = 128;                       // reduction bytes of a step
 constexpr int kFfnMaxWidth = 1 << 20;
 constexpr int kFfnFewRows = 4;                          // rows up to which k_ffn_few runs
-
-template <typename T>
-constexpr int ffn_bk() { return kFfnRowBytes / (int)sizeof(T); }
-
-typedef __bf16 fbf16x8 __attribute__((ext_vector_type(8)));
-typedef short fs16x4 __attribute__((ext_vector_type(4)));
 
 // ---------------------------------------------------------------------------
 // activations
@@ -93,228 +83,6 @@ __device__ __forceinline__ void with_act(int act, F f) {
     }
 }
 
-// ---------------------------------------------------------------------------
-// operands
-// ---------------------------------------------------------------------------
-// One side of a product: `rows` outputs by k reduction elements, element (r, k) at p[r ld + k] (KC)
-// or p[k ld + r] (MC).  Rows and reduction elements behind the end read as 0.  SPLIT: the tile's rows
-// [0, R / 2) come from p and the others from p2 (both from row 0 on).
-template <typename T>
-struct Side {
-    const T* p;
-    const T* p2;
-    int64_t ld;
-    int64_t rows;
-    int64_t k;
-};
-
-// A thread's share of a tile of R rows by one step, through registers into LDS.
-template <typename T, bool KC, int R, bool SPLIT>
-struct TileCopy {
-    static constexpr int V = 16 / sizeof(T), BK = ffn_bk<T>();
-    static constexpr int N = R * kFfnRowBytes / 16 / kFfnThreads;   // 16-byte pieces a thread
-    static constexpr int PER = KC ? BK / V : R / V;                 // pieces of a row (KC) or of a reduction element
-    static_assert(N >= 1 && kFfnThreads % PER == 0, "tile");
-    typedef typename RowVec<T>::Raw Raw;
-
-    const T* base;      // element (0, 0) of the thread's side
-    int64_t ld;
-    int line, at;       // first row (KC) or reduction element (MC), and the piece's first element across
-    int64_t across;     // MC: elements from `at` to the rows' end
-    int lim;            // KC: valid lines
-    Raw r[N];
-
-    __device__ __forceinline__ void start(const Side<T>& s) {
-        const int c = threadIdx.x % PER;
-        line = threadIdx.x / PER;
-        at = c * V;
-        base = s.p;
-        ld = s.ld;
-        if (KC) {
-            lim = (int)(s.rows < R ? s.rows : R);
-            across = 0;
-        } else {
-            int col = at;
-            if (SPLIT && at >= R / 2) {
-                base = s.p2;
-                col -= R / 2;
-            }
-            across = s.rows - col;
-            if (SPLIT && across > R / 2 - col) across = R / 2 - col;
-            base += col;
-            lim = 0;
-        }
-    }
-    // the step at reduction element k0
-    __device__ __forceinline__ void fetch(int64_t k0, int64_t k) {
-        constexpr int DL = kFfnThreads / PER;   // lines between a thread's pieces
-        if (KC) {
-            const T* b = base + k0 + at;
-            const int64_t left = k - k0 - at;
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const int row = line + j * DL;
-                r[j] = load_vec<T, true>(b + (int64_t)row * ld, row < lim ? left : 0);
-            }
-        } else {
-            const T* b = base + k0 * ld;
-            const int kl = (int)(k - k0 < BK ? k - k0 : BK);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const int kk = line + j * DL;
-                r[j] = load_vec<T, true>(b + (int64_t)kk * ld, kk < kl ? across : 0);
-            }
-        }
-    }
-    __device__ __forceinline__ void put(uint8_t* lds) const {
-        constexpr int DL = kFfnThreads / PER;
-        const int c = threadIdx.x % PER;
-#pragma unroll
-        for (int j = 0; j < N; ++j) {
-            const int row = line + j * DL;
-            *reinterpret_cast<uint4*>(lds + place(row, c)) = uint4{r[j][0], r[j][1], r[j][2], r[j][3]};
-        }
-    }
-    // Byte of piece c of a line.  KC: lines of 128 bytes, pieces permuted by the row modulo 8, so the
-    // eight rows that a read serves together lie in distinct banks.  MC bfloat16: 32-byte pairs of pieces
-    // permuted by bits 0, 1 and 3 of the reduction element (the eight that a transpose read serves
-    // together); float32: 64-byte groups permuted by bits 2 and 3.
-    static __device__ __forceinline__ int place(int row, int c) {
-        if (KC) return row * kFfnRowBytes + ((c ^ (row & 7)) * 16);
-        if constexpr (sizeof(T) == 2) {
-            constexpr int M = PER / 2 - 1;   // pairs of a line - 1
-            return row * (R * 2) + (((c >> 1) ^ (((row & 3) | ((row >> 1) & 4)) & M)) * 32) + (c & 1) * 16;
-        } else {
-            constexpr int M = PER / 4 - 1;
-            return row * (R * 4) + (((c >> 2) ^ ((row >> 2) & 3 & M)) * 64) + (c & 3) * 16;
-        }
-    }
-};
-
-// Fragment reads of one wave: operand of 16 rows from row0, reduction elements of group kk (32 of
-// bfloat16, 16 of float32) of the step; lane (i, q) holds row i, elements 8 q .. 8 q + 7 (bfloat16)
-// or 4 q .. 4 q + 3 (float32).
-template <typename T, bool KC, int R>
-struct Frag;
-template <bool KC, int R>
-struct Frag<uint16_t, KC, R> {
-    typedef fbf16x8 Reg;
-    static __device__ __forceinline__ Reg read(const uint8_t* lds, int row0, int kk) {
-        const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
-        if constexpr (KC) {
-            const int row = row0 + i;
-            return *reinterpret_cast<const fbf16x8*>(lds + row * kFfnRowBytes + (((kk * 4 + q) ^ (row & 7)) * 16));
-        } else {
-            // 8-byte piece i % 4 of the 16 rows, at reduction elements 8 q + i / 4 and four further
-            const int k0 = kk * 32 + 8 * q + (i >> 2);
-            constexpr int M = R / 16 - 1;
-            const int x = ((k0 & 3) | ((k0 >> 1) & 4)) & M;
-            const int at = k0 * (R * 2) + (((row0 >> 4) ^ x) * 32) + 8 * (i & 3);
-            typedef __attribute__((address_space(3))) fs16x4* P;
-            const fs16x4 v[2] = {__builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at)),
-                                 __builtin_amdgcn_ds_read_tr16_b64_v4i16((P)(lds + at + 4 * R * 2))};
-            return __builtin_bit_cast(fbf16x8, v);
-        }
-    }
-    static __device__ __forceinline__ floatx4 mma(const Reg& a, const Reg& b, floatx4 c) {
-        return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
-    }
-};
-template <bool KC, int R>
-struct Frag<float, KC, R> {
-    typedef floatx4 Reg;
-    static __device__ __forceinline__ Reg read(const uint8_t* lds, int row0, int kk) {
-        const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
-        if constexpr (KC) {
-            const int row = row0 + i;
-            return *reinterpret_cast<const floatx4*>(lds + row * kFfnRowBytes + (((kk * 4 + q) ^ (row & 7)) * 16));
-        } else {
-            constexpr int M = R / 16 - 1;
-            floatx4 v;
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const int k = kk * 16 + 4 * q + s;
-                v[s] = *reinterpret_cast<const float*>(lds + k * (R * 4) + (((row0 >> 4) ^ (q & M)) * 64) + i * 4);
-            }
-            return v;
-        }
-    }
-    static __device__ __forceinline__ floatx4 mma(const Reg& a, const Reg& b, floatx4 c) {
-#pragma unroll
-        for (int s = 0; s < 4; ++s) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a[s], b[s], c, 0, 0, 0);
-        return c;
-    }
-};
-
-// LDS of a block: two stages of both operands.
-template <int MT, int NT>
-constexpr int ffn_lds() { return 2 * 32 * (MT + NT) * kFfnRowBytes; }
-
-// acc[mi][ni] += the tile's product.  Four waves, (wm, wn) = 2 x 2: wave rows 16 MT wm .., columns
-// 16 NT wn .. (SPLIT: half of them from either half of the tile's columns).  The second operand goes
-// into the MFMA first, so lane (i, q) gets row 16 mi + i of its rows and four consecutive columns 4 q ..
-// of block ni.  LDS may be in use by other waves' earlier reads: starts with a barrier.
-template <typename T, bool AKC, bool BKC, int MT, int NT, bool SPLIT>
-__device__ __forceinline__ void tile_product(const Side<T>& A, const Side<T>& B, uint8_t* lds, floatx4 (&acc)[MT][NT]) {
-    constexpr int RA = 32 * MT, RB = 32 * NT, BK = ffn_bk<T>();
-    constexpr int STAGE = (RA + RB) * kFfnRowBytes;
-    typedef Frag<T, AKC, RA> FA;
-    typedef Frag<T, BKC, RB> FB;
-    TileCopy<T, AKC, RA, false> ca;
-    TileCopy<T, BKC, RB, SPLIT> cb;
-    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-    const int64_t K = A.k;
-    ca.start(A);
-    cb.start(B);
-    ca.fetch(0, K);
-    cb.fetch(0, B.k);
-    __syncthreads();
-    ca.put(lds);
-    cb.put(lds + RA * kFfnRowBytes);
-    __syncthreads();
-    int cur = 0;
-    for (int64_t k0 = 0; k0 < K; k0 += BK) {
-        const bool more = k0 + BK < K;
-        if (more) {
-            ca.fetch(k0 + BK, K);
-            cb.fetch(k0 + BK, B.k);
-        }
-        const uint8_t* la = lds + cur * STAGE;
-        const uint8_t* lb = la + RA * kFfnRowBytes;
-#pragma unroll
-        for (int kk = 0; kk < 2; ++kk) {
-            typename FA::Reg a[MT], b[NT];
-#pragma unroll
-            for (int mi = 0; mi < MT; ++mi) a[mi] = FA::read(la, 16 * (MT * wm + mi), kk);
-#pragma unroll
-            for (int ni = 0; ni < NT; ++ni) {
-                const int col = !SPLIT ? 16 * (NT * wn + ni)
-                                       : 16 * (NT / 2 * wn + ni % (NT / 2)) + (ni < NT / 2 ? 0 : RB / 2);
-                b[ni] = FB::read(lb, col, kk);
-            }
-#pragma unroll
-            for (int mi = 0; mi < MT; ++mi)
-#pragma unroll
-                for (int ni = 0; ni < NT; ++ni) acc[mi][ni] = FA::mma(b[ni], a[mi], acc[mi][ni]);
-        }
-        if (more) {
-            cur ^= 1;
-            uint8_t* ld = lds + cur * STAGE;
-            ca.put(ld);
-            cb.put(ld + RA * kFfnRowBytes);
-        }
-        __syncthreads();
-    }
-}
-
-template <int MT, int NT>
-__device__ __forceinline__ void zero_acc(floatx4 (&acc)[MT][NT]) {
-#pragma unroll
-    for (int a = 0; a < MT; ++a)
-#pragma unroll
-        for (int b = 0; b < NT; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
-}
-
 // four consecutive columns of a row
 __device__ __forceinline__ void store4(float* p, int64_t left, const float (&v)[4]) {
     if (left >= 4) {
@@ -337,30 +105,49 @@ __device__ __forceinline__ void store4(uint16_t* p, int64_t left, const float (&
 }
 
 // ---------------------------------------------------------------------------
-// kernels
+// what happens to a tile's sums: lane (i, q) of a wave holds row 16 mi + i of its rows and columns 16 ni + 4 q ..
+// of its columns
 // ---------------------------------------------------------------------------
-// H (n x ldh, columns behind f zero) of a tile of 32 MT rows by 64 hidden columns.
+__device__ __forceinline__ int ffn_i() { return threadIdx.x & 15; }
+__device__ __forceinline__ int ffn_q() { return (threadIdx.x & 63) >> 4; }
+
+template <int MT, int NT>
+__device__ __forceinline__ void zero_acc(floatx4 (&acc)[MT][NT]) {
+#pragma unroll
+    for (int a = 0; a < MT; ++a)
+#pragma unroll
+        for (int b = 0; b < NT; ++b) acc[a][b] = floatx4{0.f, 0.f, 0.f, 0.f};
+}
+
+// the sums themselves, to rows below n and columns below nn
+template <typename T, int MT, int NT>
+__device__ __forceinline__ void store_tile(const floatx4 (&acc)[MT][NT], int64_t row0, int64_t col0, int64_t n, int64_t nn,
+                                           T* __restrict__ out, int64_t ld) {
+#pragma unroll
+    for (int mi = 0; mi < MT; ++mi) {
+        const int64_t row = row0 + 16 * mi + ffn_i();
+        if (row >= n) continue;
+#pragma unroll
+        for (int ni = 0; ni < NT; ++ni) {
+            const int64_t col = col0 + 16 * ni + 4 * ffn_q();
+            const float v[4] = {acc[mi][ni][0], acc[mi][ni][1], acc[mi][ni][2], acc[mi][ni][3]};
+            if (col < nn) store4(out + row * ld + col, nn - col, v);
+        }
+    }
+}
+
+// H from gates (blocks 0, 1) and their partners (blocks 2, 3)
 template <typename T, int MT>
-__global__ void __launch_bounds__(kFfnThreads, 2)
-k_ffn_up(const T* __restrict__ X, int64_t n, int ci, const T* __restrict__ Wg, const T* __restrict__ Wu, int f, int act,
-         T* __restrict__ H, int64_t ldh, int nf) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<MT, 4>()];
-    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
-    const int64_t r0 = u / nf * (32 * MT);
-    const int c0 = (int)(u % nf) * 64;
-    floatx4 acc[MT][4];
-    zero_acc(acc);
-    tile_product<T, true, false, MT, 4, true>({X + r0 * ci, nullptr, ci, n - r0, ci},
-                                              {Wg + c0, Wu + c0, f, f - c0, ci}, lds, acc);
-    const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, i = threadIdx.x & 15, q = (threadIdx.x & 63) >> 4;
+__device__ __forceinline__ void store_hidden(const floatx4 (&acc)[MT][4], int64_t row0, int64_t col0, int64_t n, int act,
+                                             T* __restrict__ H, int64_t ldh) {
     with_act(act, [&](auto ACT) {
 #pragma unroll
         for (int mi = 0; mi < MT; ++mi) {
-            const int64_t row = r0 + 16 * (MT * wm + mi) + i;
+            const int64_t row = row0 + 16 * mi + ffn_i();
             if (row >= n) continue;
 #pragma unroll
             for (int ni = 0; ni < 2; ++ni) {
-                const int col = c0 + 16 * (2 * wn + ni) + 4 * q;
+                const int64_t col = col0 + 16 * ni + 4 * ffn_q();
                 float h[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -374,66 +161,19 @@ k_ffn_up(const T* __restrict__ X, int64_t n, int ci, const T* __restrict__ Wg, c
     });
 }
 
-// Out (n x co) = A1 B1 (+ A2 B2 where A2 is given): A rows of the reduction (KC), B either way.
-template <typename T, bool BKC, int MT, int NT>
-__global__ void __launch_bounds__(kFfnThreads, 2)
-k_ffn_gemm(const T* __restrict__ A1, const T* __restrict__ A2, int64_t lda, int64_t n, int64_t ka,
-           const T* __restrict__ B1, const T* __restrict__ B2, int64_t ldb, int64_t kb, int co, T* __restrict__ Out,
-           int nc) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<MT, NT>()];
-    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
-    const int64_t r0 = u / nc * (32 * MT);
-    const int c0 = (int)(u % nc) * (32 * NT);
-    floatx4 acc[MT][NT];
-    zero_acc(acc);
-    for (int s = 0; s < 2; ++s) {
-        const T* A = s ? A2 : A1;
-        const T* B = s ? B2 : B1;
-        if (!A) break;
-        tile_product<T, true, BKC, MT, NT, false>(
-            {A + r0 * lda, nullptr, lda, n - r0, ka},
-            {BKC ? B + (int64_t)c0 * ldb : B + c0, nullptr, ldb, co - c0, kb}, lds, acc);
-    }
-    const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, i = threadIdx.x & 15, q = (threadIdx.x & 63) >> 4;
-#pragma unroll
-    for (int mi = 0; mi < MT; ++mi) {
-        const int64_t row = r0 + 16 * (MT * wm + mi) + i;
-        if (row >= n) continue;
-#pragma unroll
-        for (int ni = 0; ni < NT; ++ni) {
-            const int col = c0 + 16 * (NT * wn + ni) + 4 * q;
-            const float v[4] = {acc[mi][ni][0], acc[mi][ni][1], acc[mi][ni][2], acc[mi][ni][3]};
-            if (col < co) store4(Out + row * co + col, co - col, v);
-        }
-    }
-}
-
-// H (n x f8) and dG, dU (n x 2 f8, side by side) of a tile of 32 MT rows by 64 hidden columns.
+// H, and dG and dU side by side, from gates, partners and dH
 template <typename T, int MT>
-__global__ void __launch_bounds__(kFfnThreads, 2)
-k_ffn_mid(const T* __restrict__ X, const T* __restrict__ dY, int64_t n, int ci, int co, const T* __restrict__ Wg,
-          const T* __restrict__ Wu, const T* __restrict__ Wd, int f, int act, T* __restrict__ H, T* __restrict__ dGU,
-          int f8, int nf) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<MT, 4>()];
-    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
-    const int64_t r0 = u / nf * (32 * MT);
-    const int c0 = (int)(u % nf) * 64;
-    floatx4 acc[MT][4], dh[MT][2];
-    zero_acc(acc);
-    zero_acc(dh);
-    tile_product<T, true, false, MT, 4, true>({X + r0 * ci, nullptr, ci, n - r0, ci},
-                                              {Wg + c0, Wu + c0, f, f - c0, ci}, lds, acc);
-    tile_product<T, true, true, MT, 2, false>({dY + r0 * co, nullptr, co, n - r0, co},
-                                              {Wd + (int64_t)c0 * co, nullptr, co, f - c0, co}, lds, dh);
-    const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, i = threadIdx.x & 15, q = (threadIdx.x & 63) >> 4;
+__device__ __forceinline__ void store_mid(const floatx4 (&acc)[MT][4], const floatx4 (&dh)[MT][2], int64_t row0,
+                                          int64_t col0, int64_t n, int act, T* __restrict__ H, T* __restrict__ dGU,
+                                          int64_t f8) {
     with_act(act, [&](auto ACT) {
 #pragma unroll
         for (int mi = 0; mi < MT; ++mi) {
-            const int64_t row = r0 + 16 * (MT * wm + mi) + i;
+            const int64_t row = row0 + 16 * mi + ffn_i();
             if (row >= n) continue;
 #pragma unroll
             for (int ni = 0; ni < 2; ++ni) {
-                const int col = c0 + 16 * (2 * wn + ni) + 4 * q;
+                const int64_t col = col0 + 16 * ni + 4 * ffn_q();
                 float h[4], dg[4], du[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
@@ -444,13 +184,73 @@ k_ffn_mid(const T* __restrict__ X, const T* __restrict__ dY, int64_t n, int ci, 
                     dg[e] = g * up * d;
                     du[e] = g * a;
                 }
-                const int64_t left = f8 - col;
-                store4(H + row * f8 + col, left, h);
-                store4(dGU + row * 2 * f8 + col, left, dg);
-                store4(dGU + row * 2 * f8 + f8 + col, left, du);
+                store4(H + row * f8 + col, f8 - col, h);
+                store4(dGU + row * 2 * f8 + col, f8 - col, dg);
+                store4(dGU + row * 2 * f8 + f8 + col, f8 - col, du);
             }
         }
     });
+}
+
+// ---------------------------------------------------------------------------
+// float32 kernels: tiles of 32 MT rows
+// ---------------------------------------------------------------------------
+// H (n x ldh, columns behind f zero) of a tile by 64 hidden columns.
+template <int MT>
+__global__ void __launch_bounds__(kFfnThreads, 2)
+k_ffn_up_f32(const float* __restrict__ X, int64_t n, int ci, const float* __restrict__ Wg, const float* __restrict__ Wu,
+             int f, int act, float* __restrict__ H, int64_t ldh, int nf) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<MT, 4>()];
+    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
+    const int64_t r0 = u / nf * (32 * MT);
+    const int c0 = (int)(u % nf) * 64, wave = threadIdx.x >> 6;
+    floatx4 acc[MT][4];
+    zero_acc(acc);
+    tile_product<true, false, MT, 4, true>({X + r0 * ci, nullptr, ci, n - r0, ci}, {Wg + c0, Wu + c0, f, f - c0, ci},
+                                           lds, acc);
+    store_hidden(acc, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H, ldh);
+}
+
+// Out (n x co) = A1 B1 (+ A2 B2 where A2 is given): A rows of the reduction (KC), B either way.
+template <bool BKC, int MT, int NT>
+__global__ void __launch_bounds__(kFfnThreads, 2)
+k_ffn_gemm_f32(const float* __restrict__ A1, const float* __restrict__ A2, int64_t lda, int64_t n, int64_t ka,
+               const float* __restrict__ B1, const float* __restrict__ B2, int64_t ldb, int64_t kb, int co,
+               float* __restrict__ Out, int nc) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<MT, NT>()];
+    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
+    const int64_t r0 = u / nc * (32 * MT);
+    const int c0 = (int)(u % nc) * (32 * NT), wave = threadIdx.x >> 6;
+    floatx4 acc[MT][NT];
+    zero_acc(acc);
+    for (int s = 0; s < 2; ++s) {
+        const float* A = s ? A2 : A1;
+        const float* B = s ? B2 : B1;
+        if (!A) break;
+        tile_product<true, BKC, MT, NT, false>({A + r0 * lda, nullptr, lda, n - r0, ka},
+                                               {BKC ? B + (int64_t)c0 * ldb : B + c0, nullptr, ldb, co - c0, kb}, lds, acc);
+    }
+    store_tile(acc, r0 + 16 * MT * (wave >> 1), c0 + 16 * NT * (wave & 1), n, co, Out, co);
+}
+
+// H (n x f8) and dG, dU (n x 2 f8, side by side) of a tile by 64 hidden columns.
+template <int MT>
+__global__ void __launch_bounds__(kFfnThreads, 2)
+k_ffn_mid_f32(const float* __restrict__ X, const float* __restrict__ dY, int64_t n, int ci, int co,
+              const float* __restrict__ Wg, const float* __restrict__ Wu, const float* __restrict__ Wd, int f, int act,
+              float* __restrict__ H, float* __restrict__ dGU, int f8, int nf) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<MT, 4>()];
+    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
+    const int64_t r0 = u / nf * (32 * MT);
+    const int c0 = (int)(u % nf) * 64, wave = threadIdx.x >> 6;
+    floatx4 acc[MT][4], dh[MT][2];
+    zero_acc(acc);
+    zero_acc(dh);
+    tile_product<true, false, MT, 4, true>({X + r0 * ci, nullptr, ci, n - r0, ci}, {Wg + c0, Wu + c0, f, f - c0, ci},
+                                           lds, acc);
+    tile_product<true, true, MT, 2, false>({dY + r0 * co, nullptr, co, n - r0, co},
+                                           {Wd + (int64_t)c0 * co, nullptr, co, f - c0, co}, lds, dh);
+    store_mid(acc, dh, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H, dGU, f8);
 }
 
 // One product of k_ffn_dw: out (m x nn) = A^T B over the rows, A n x lda, B n x ldb.
@@ -465,36 +265,153 @@ struct DwSide {
 };
 
 // Partial sums of both products over the rows of a chunk.
-template <typename T, int MT, int NT>
+template <int MT, int NT>
 __global__ void __launch_bounds__(kFfnThreads, 2)
-k_ffn_dw(DwSide<T> p0, DwSide<T> p1, int64_t n, int64_t chunk, int64_t per_chunk, float* __restrict__ part) {
+k_ffn_dw_f32(DwSide<float> p0, DwSide<float> p1, int64_t n, int64_t chunk, int64_t per_chunk, float* __restrict__ part) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<MT, NT>()];
     const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
     const int tiles = p0.tiles + p1.tiles;
     const int64_t s = u / tiles;
     int t = (int)(u - s * tiles);
     const bool second = t >= p0.tiles;
-    const DwSide<T> p = second ? p1 : p0;
+    const DwSide<float> p = second ? p1 : p0;
     if (second) t -= p0.tiles;
-    const int m0 = t / p.tn * (32 * MT), c0 = t % p.tn * (32 * NT);
+    const int m0 = t / p.tn * (32 * MT), c0 = t % p.tn * (32 * NT), wave = threadIdx.x >> 6;
     const int64_t r0 = s * chunk, rows = n - r0 < chunk ? n - r0 : chunk;
     floatx4 acc[MT][NT];
     zero_acc(acc);
-    tile_product<T, false, false, MT, NT, false>({p.A + r0 * p.lda + m0, nullptr, p.lda, p.m - m0, rows},
-                                                 {p.B + r0 * p.ldb + c0, nullptr, p.ldb, p.nn - c0, rows}, lds, acc);
-    const int wave = threadIdx.x >> 6, wm = wave >> 1, wn = wave & 1, i = threadIdx.x & 15, q = (threadIdx.x & 63) >> 4;
-    float* out = part + s * per_chunk + p.part;
+    tile_product<false, false, MT, NT, false>({p.A + r0 * p.lda + m0, nullptr, p.lda, p.m - m0, rows},
+                                              {p.B + r0 * p.ldb + c0, nullptr, p.ldb, p.nn - c0, rows}, lds, acc);
+    store_tile(acc, m0 + 16 * MT * (wave >> 1), c0 + 16 * NT * (wave & 1), p.m, p.nn, part + s * per_chunk + p.part, p.nn);
+}
+
+// ---------------------------------------------------------------------------
+// bfloat16 kernels: operands with rows of whole 16-byte pieces (ld: their strides)
+// ---------------------------------------------------------------------------
+// Copies of up to five matrices with their rows padded to whole pieces.
+struct FfnPad {
+    const uint16_t* src[5];
+    uint16_t* dst[5];
+    int cols[5], ld[5];
+    int64_t end[5];   // pieces of the matrices up to and with this one
+    int count;
+};
+__global__ void __launch_bounds__(kFfnThreads) k_ffn_pad(FfnPad p) {
+    const int64_t total = p.end[p.count - 1];
+    for (int64_t i = (int64_t)blockIdx.x * kFfnThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kFfnThreads) {
+        const uint16_t* src = p.src[0];
+        uint16_t* dst = p.dst[0];
+        int cols = p.cols[0], ld = p.ld[0];
+        int64_t at = i;
 #pragma unroll
-    for (int mi = 0; mi < MT; ++mi) {
-        const int row = m0 + 16 * (MT * wm + mi) + i;
-        if (row >= p.m) continue;
-#pragma unroll
-        for (int ni = 0; ni < NT; ++ni) {
-            const int col = c0 + 16 * (NT * wn + ni) + 4 * q;
-            const float v[4] = {acc[mi][ni][0], acc[mi][ni][1], acc[mi][ni][2], acc[mi][ni][3]};
-            if (col < p.nn) store4(out + (int64_t)row * p.nn + col, p.nn - col, v);
-        }
+        for (int m = 1; m < 5; ++m)
+            if (m < p.count && i >= p.end[m - 1]) {
+                src = p.src[m];
+                dst = p.dst[m];
+                cols = p.cols[m];
+                ld = p.ld[m];
+                at = i - p.end[m - 1];
+            }
+        const int64_t row = at / (ld / 8);
+        const int c = (int)(at - row * (ld / 8)) * 8;
+        const RowVec<uint16_t>::Raw v = load_vec<uint16_t, true>(src + row * cols + c, cols - c);
+        *reinterpret_cast<uint4*>(dst + at * 8) = uint4{v[0], v[1], v[2], v[3]};
     }
+}
+
+// H (n x ldh) of a tile of 32 MT rows by 64 hidden columns.
+template <int MT>
+__global__ void __launch_bounds__(256, 2)
+k_ffn_up_bf16(const uint16_t* __restrict__ X, int64_t ldx, int64_t n, int ci, const uint16_t* __restrict__ Wg,
+              const uint16_t* __restrict__ Wu, int64_t ldw, int f, int act, uint16_t* __restrict__ H, int64_t ldh, int nf) {
+    typedef FbShape<2, 2, MT, 4> S;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
+    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
+    const int64_t r0 = u / nf * S::BM;
+    const int c0 = (int)(u % nf) * 64, wave = threadIdx.x >> 6;
+    floatx4 acc[MT][4];
+    zero_acc(acc);
+    fb_product<2, 2, MT, 4, false, FB_PAIR>({X + r0 * ldx, ldx, n - r0}, {Wg + c0, ldw, f - c0}, Wu + c0, ci, lds, acc);
+    store_hidden(acc, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H, ldh);
+}
+
+// Out (n x co, rows as they are) = A1 B1 (+ A2 B2 where A2 is given) over k.
+template <int WM, int WN, int MT, FbB BK>
+__global__ void __launch_bounds__(256, 2)
+k_ffn_gemm_bf16(const uint16_t* __restrict__ A1, const uint16_t* __restrict__ A2, int64_t lda, int64_t n, int64_t k,
+                const uint16_t* __restrict__ B1, const uint16_t* __restrict__ B2, int64_t ldb, int co,
+                uint16_t* __restrict__ Out, int nc) {
+    typedef FbShape<WM, WN, MT, 4> S;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
+    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
+    const int64_t r0 = u / nc * S::BM;
+    const int c0 = (int)(u % nc) * S::BN, wave = threadIdx.x >> 6;
+    floatx4 acc[MT][4];
+    zero_acc(acc);
+    for (int s = 0; s < 2; ++s) {
+        const uint16_t* A = s ? A2 : A1;
+        const uint16_t* B = s ? B2 : B1;
+        if (!A) break;
+        if (s) fb_barrier();   // the first product's last reads
+        fb_product<WM, WN, MT, 4, false, BK>({A + r0 * lda, lda, n - r0},
+                                             {BK == FB_KC ? B + (int64_t)c0 * ldb : B + c0, ldb, co - c0}, nullptr, k, lds,
+                                             acc);
+    }
+    store_tile(acc, r0 + 16 * MT * (wave / WN), c0 + 64 * (wave % WN), n, co, Out, co);
+}
+
+// H (n x f8) and dG, dU (n x 2 f8, side by side) of a tile of 128 rows by 64 hidden columns.
+template <int MT>
+__global__ void __launch_bounds__(256, 2)
+k_ffn_mid_bf16(const uint16_t* __restrict__ X, int64_t ldx, const uint16_t* __restrict__ dY, int64_t ldy, int64_t n, int ci,
+               int co, const uint16_t* __restrict__ Wg, const uint16_t* __restrict__ Wu, int64_t ldw,
+               const uint16_t* __restrict__ Wd, int64_t ldd, int f, int act, uint16_t* __restrict__ H,
+               uint16_t* __restrict__ dGU, int f8, int nf) {
+    typedef FbShape<2, 2, MT, 4> S;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
+    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
+    const int64_t r0 = u / nf * S::BM;
+    const int c0 = (int)(u % nf) * 64, wave = threadIdx.x >> 6;
+    floatx4 acc[MT][4], dh[MT][2];
+    zero_acc(acc);
+    zero_acc(dh);
+    fb_product<2, 2, MT, 4, false, FB_PAIR>({X + r0 * ldx, ldx, n - r0}, {Wg + c0, ldw, f - c0}, Wu + c0, ci, lds, acc);
+    fb_barrier();
+    fb_product<2, 2, MT, 2, false, FB_KC>({dY + r0 * ldy, ldy, n - r0}, {Wd + (int64_t)c0 * ldd, ldd, f - c0}, nullptr, co,
+                                          lds, dh);
+    store_mid(acc, dh, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H, dGU, f8);
+}
+
+template <int WM, int WN, int MT>
+__device__ __forceinline__ void dw_tile(const DwSide<uint16_t>& p, int t, int64_t r0, int64_t rows, uint8_t* lds,
+                                        float* __restrict__ part) {
+    typedef FbShape<WM, WN, MT, 4> S;
+    const int m0 = t / p.tn * S::BM, c0 = t % p.tn * S::BN, wave = threadIdx.x >> 6;
+    floatx4 acc[MT][4];
+    zero_acc(acc);
+    fb_product<WM, WN, MT, 4, true, FB_MC>({p.A + r0 * p.lda + m0, p.lda, p.m - m0},
+                                           {p.B + r0 * p.ldb + c0, p.ldb, p.nn - c0}, nullptr, rows, lds, acc);
+    store_tile(acc, m0 + 16 * MT * (wave / WN), c0 + 64 * (wave % WN), p.m, p.nn, part + p.part, p.nn);
+}
+
+// Partial sums of both products over the rows of a chunk: the first in tiles of 16 MT0 x 256 (its rows are the
+// channels), the second in tiles of 256 x 128 or, NARROW, 256 x 64 (its columns are).
+template <int MT0, bool NARROW>
+__global__ void __launch_bounds__(256, 2)
+k_ffn_dw_bf16(DwSide<uint16_t> p0, DwSide<uint16_t> p1, int64_t n, int64_t chunk, int64_t per_chunk,
+              float* __restrict__ part) {
+    constexpr int MT1 = NARROW ? 4 : 8, WM1 = NARROW ? 4 : 2, WN1 = NARROW ? 1 : 2;
+    typedef FbShape<1, 4, MT0, 4> S0;
+    typedef FbShape<WM1, WN1, MT1, 4> S1;
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[S0::LDS > S1::LDS ? S0::LDS : S1::LDS];
+    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
+    const int tiles = p0.tiles + p1.tiles;
+    const int64_t s = u / tiles;
+    const int t = (int)(u - s * tiles);
+    const int64_t r0 = s * chunk, rows = n - r0 < chunk ? n - r0 : chunk;
+    float* out = part + s * per_chunk;
+    if (t < p0.tiles) dw_tile<1, 4, MT0>(p0, t, r0, rows, lds, out);
+    else dw_tile<WM1, WN1, MT1>(p1, t - p0.tiles, r0, rows, lds, out);
 }
 
 // The weights' gradients from the chunks' sums, added in chunk order: per chunk dWg | dWu as ci x 2 f8, then dWd.
@@ -529,10 +446,10 @@ k_ffn_dw_sum(const float* __restrict__ part, int64_t chunks, int64_t per_chunk, 
 // columns, so that even a narrow layer is spread over many blocks.
 constexpr int kFewCols = 4, kFewLanes = kFfnThreads / kFewCols;
 
-template <typename T, int R, bool GATED>
+template <typename TA, typename T, typename TO, int R, bool GATED>
 __global__ void __launch_bounds__(kFfnThreads)
-k_ffn_few(const T* __restrict__ A, int64_t lda, int n, int k, const T* __restrict__ B, const T* __restrict__ B2, int nn,
-          int act, T* __restrict__ out, int64_t ldo) {
+k_ffn_few(const TA* __restrict__ A, int64_t lda, int n, int k, const T* __restrict__ B, const T* __restrict__ B2, int nn,
+          int act, TO* __restrict__ out, int64_t ldo) {
     typedef RowVec<T> RV;
     constexpr int V = RV::V, NB = GATED ? 2 : 1;
     __shared__ float red[kFfnThreads / 64][NB * R * V * kFewCols];
@@ -598,54 +515,32 @@ k_ffn_few(const T* __restrict__ A, int64_t lda, int n, int k, const T* __restric
 static int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 static int64_t pad8(int64_t v) { return (v + 7) / 8 * 8; }
 static size_t ffn_al256(size_t b) { return (b + 255) & ~(size_t)255; }
-static size_t ffn_size(int dtype) { return dtype == GSC_BF16 ? 2 : 4; }
-
-// 16-row blocks a wave takes in a direction of `rows` outputs: 4 (tiles of 128) unless tiles of 64 leave
-// less of the last one empty.
-static bool ffn_narrow(int64_t rows) { return ceil_div(rows, 64) % 2 == 1 && rows < 512; }
 
 static bool ffn_sizes_ok(int32_t dtype, int64_t n, int32_t ci, int32_t f, int32_t co) {
     return (dtype == GSC_F32 || dtype == GSC_BF16) && n >= 0 && ci >= 1 && f >= 1 && co >= 1 && ci <= kFfnMaxWidth &&
            f <= kFfnMaxWidth && co <= kFfnMaxWidth && n <= ((int64_t)1 << 31) * 16;
 }
 
-// Row tiles of 64 where 128 would leave compute units idle.
-static bool ffn_short(int64_t n, int64_t col_tiles) { return ceil_div(n, 128) * col_tiles < 2 * device_cus(); }
+struct FfnShape {
+    int64_t n;
+    int ci, f, co;
+    int64_t f8;
+    FfnShape(int64_t n, int ci, int f, int co) : n(n), ci(ci), f(f), co(co), f8(pad8(f)) {}
+};
 
-template <typename T, bool BKC>
-static void ffn_gemm(const T* A1, const T* A2, int64_t lda, int64_t n, int64_t ka, const T* B1, const T* B2, int64_t ldb,
-                     int64_t kb, int co, T* Out, hipStream_t s) {
-    const bool nar = ffn_narrow(co);
-    const int nc = (int)ceil_div(co, nar ? 64 : 128);
-    const bool sho = ffn_short(n, nc);
-    auto* kern = sho ? (nar ? k_ffn_gemm<T, BKC, 2, 2> : k_ffn_gemm<T, BKC, 2, 4>)
-                     : (nar ? k_ffn_gemm<T, BKC, 4, 2> : k_ffn_gemm<T, BKC, 4, 4>);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(n, sho ? 64 : 128) * nc)), dim3(kFfnThreads), 0, s, A1, A2, lda,
-                       n, ka, B1, B2, ldb, kb, co, Out, nc);
-}
+// Workspace, in order: what the padded copies of X, dY (backward), Wg, Wu and Wd take (bfloat16), H, then for the
+// backward pass dG | dU and the weight gradients' partial sums.
+struct FfnLayout {
+    size_t x, dy, wg, wu, wd, h, dgu, part, total;
+    int64_t per_chunk, up, chunks, chunk;
+    bool m_nar, n_nar;      // tiles of 64 channels for the weight gradients of the first, of the second projection
+    int tn0, t0, tn1, t1;
+};
 
-template <typename T>
-static void ffn_fwd(const T* X, int64_t n, int ci, const T* Wg, const T* Wu, int f, const T* Wd, int co, int act, T* Y,
-                    T* H, hipStream_t s) {
-    const int64_t f8 = pad8(f);
-    if (n <= kFfnFewRows) {
-        constexpr int W = kFewCols * (16 / (int)sizeof(T));
-        auto* up = n == 1 ? k_ffn_few<T, 1, true> : (n == 2 ? k_ffn_few<T, 2, true> : k_ffn_few<T, 4, true>);
-        auto* down = n == 1 ? k_ffn_few<T, 1, false> : (n == 2 ? k_ffn_few<T, 2, false> : k_ffn_few<T, 4, false>);
-        hipLaunchKernelGGL(up, dim3((unsigned)ceil_div(f, W)), dim3(kFfnThreads), 0, s, X, (int64_t)ci, (int)n, ci, Wg,
-                           Wu, f, act, H, f8);
-        hipLaunchKernelGGL(down, dim3((unsigned)ceil_div(co, W)), dim3(kFfnThreads), 0, s, H, f8, (int)n, f, Wd,
-                           (const T*)nullptr, co, act, Y, (int64_t)co);
-        return;
-    }
-    const int nf = (int)ceil_div(f, 64);
-    const bool sho = ffn_short(n, nf);
-    auto* up = sho ? k_ffn_up<T, 2> : k_ffn_up<T, 4>;
-    hipLaunchKernelGGL(up, dim3((unsigned)(ceil_div(n, sho ? 64 : 128) * nf)), dim3(kFfnThreads), 0, s, X, n, ci, Wg, Wu, f, act, H, f8, nf);
-    ffn_gemm<T, false>(H, nullptr, f8, n, f8, Wd, nullptr, co, f, co, Y, s);
-}
+// float32: tiles of 64 outputs instead of 128 in a direction where they leave less of the last one empty.
+static bool ffn_narrow(int64_t rows) { return ceil_div(rows, 64) % 2 == 1 && rows < 512; }
 
-// Row chunks of the weights' gradients: enough blocks for the device, at least 512 rows each.
+// Row chunks of the weights' gradients: about four blocks a compute unit, at least 512 rows each.
 constexpr int64_t kFfnChunkRows = 512;
 static int64_t ffn_chunks(int64_t n, int64_t tiles) {
     int64_t c = ceil_div(4 * 256, tiles);
@@ -654,63 +549,210 @@ static int64_t ffn_chunks(int64_t n, int64_t tiles) {
     return c < 1 ? 1 : c;
 }
 
-struct FfnBwdLayout {
-    int64_t f8, per_chunk, up, chunks, chunk;
-    int m_nar, n_nar;   // tiles of 64 rows, of 64 columns
-    int tn0, t0, tn1, t1;
-    size_t h, dgu, part, total;
-};
-
-static FfnBwdLayout ffn_bwd_layout(int dtype, int64_t n, int ci, int f, int co) {
-    FfnBwdLayout L;
-    L.f8 = pad8(f);
-    L.m_nar = ffn_narrow(ci);
-    L.n_nar = ffn_narrow(co);
-    const int bm = L.m_nar ? 64 : 128, bn = L.n_nar ? 64 : 128;
-    L.tn0 = (int)ceil_div(2 * L.f8, bn);
-    L.t0 = (int)ceil_div(ci, bm) * L.tn0;
-    L.tn1 = (int)ceil_div(co, bn);
-    L.t1 = (int)ceil_div(f, bm) * L.tn1;
-    L.chunks = ffn_chunks(n, (int64_t)L.t0 + L.t1);
-    L.chunk = ceil_div(ceil_div(n > 0 ? n : 1, L.chunks), 64) * 64;
-    L.chunks = ceil_div(n > 0 ? n : 1, L.chunk);
-    L.up = (int64_t)ci * 2 * L.f8;
-    L.per_chunk = L.up + (int64_t)f * co;
-    L.h = 0;
-    L.dgu = ffn_al256((size_t)n * L.f8 * ffn_size(dtype));
-    L.part = L.dgu + ffn_al256((size_t)n * 2 * L.f8 * ffn_size(dtype));
-    L.total = L.part + ffn_al256((size_t)L.chunks * L.per_chunk * sizeof(float));
+static FfnLayout ffn_layout(int dtype, const FfnShape& d, bool bwd) {
+    FfnLayout L{};
+    const size_t size = dtype == GSC_BF16 ? 2 : 4;
+    size_t at = 0;
+    auto take = [&](size_t bytes) {
+        const size_t a = at;
+        at += ffn_al256(bytes);
+        return a;
+    };
+    const int64_t rows = d.n > 0 ? d.n : 1;
+    if (dtype == GSC_BF16) {
+        L.x = take((size_t)d.n * pad8(d.ci) * 2);
+        if (bwd) L.dy = take((size_t)d.n * pad8(d.co) * 2);
+        L.wg = take((size_t)d.ci * d.f8 * 2);
+        L.wu = take((size_t)d.ci * d.f8 * 2);
+        L.wd = take((size_t)d.f * pad8(d.co) * 2);
+    }
+    L.h = take((size_t)d.n * d.f8 * (d.n <= kFfnFewRows ? 4 : size));
+    if (bwd) {
+        L.dgu = take((size_t)d.n * 2 * d.f8 * size);
+        int bm0, bn0, bm1, bn1;
+        if (dtype == GSC_BF16) {
+            L.m_nar = d.ci <= 64;
+            L.n_nar = d.co <= 64;
+            bm0 = L.m_nar ? 64 : 128;
+            bn0 = bm1 = 256;
+            bn1 = L.n_nar ? 64 : 128;
+        } else {
+            L.m_nar = ffn_narrow(d.ci);
+            L.n_nar = ffn_narrow(d.co);
+            bm0 = bm1 = L.m_nar ? 64 : 128;
+            bn0 = bn1 = L.n_nar ? 64 : 128;
+        }
+        L.tn0 = (int)ceil_div(2 * d.f8, bn0);
+        L.t0 = (int)ceil_div(d.ci, bm0) * L.tn0;
+        L.tn1 = (int)ceil_div(d.co, bn1);
+        L.t1 = (int)ceil_div(d.f, bm1) * L.tn1;
+        L.chunk = ceil_div(ceil_div(rows, ffn_chunks(d.n, (int64_t)L.t0 + L.t1)), 64) * 64;
+        L.chunks = ceil_div(rows, L.chunk);
+        L.up = (int64_t)d.ci * 2 * d.f8;
+        L.per_chunk = L.up + (int64_t)d.f * d.co;
+        L.part = take((size_t)L.chunks * L.per_chunk * sizeof(float));
+    }
+    L.total = at > 0 ? at : 256;
     return L;
 }
 
+// Row tiles of 64 (float32) or 128 (bfloat16) instead of twice as many where those would leave compute units idle.
+static bool ffn_short(int64_t n, int rows, int64_t col_tiles) { return ceil_div(n, rows) * col_tiles < 2 * device_cus(); }
+
+// --- float32
+template <bool BKC>
+static void ffn_gemm_f32(const float* A1, const float* A2, int64_t lda, int64_t n, int64_t ka, const float* B1,
+                         const float* B2, int64_t ldb, int64_t kb, int co, float* Out, hipStream_t s) {
+    const bool nar = ffn_narrow(co);
+    const int nc = (int)ceil_div(co, nar ? 64 : 128);
+    const bool sho = ffn_short(n, 128, nc);
+    auto* kern = sho ? (nar ? k_ffn_gemm_f32<BKC, 2, 2> : k_ffn_gemm_f32<BKC, 2, 4>)
+                     : (nar ? k_ffn_gemm_f32<BKC, 4, 2> : k_ffn_gemm_f32<BKC, 4, 4>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(n, sho ? 64 : 128) * nc)), dim3(kFfnThreads), 0, s, A1, A2, lda,
+                       n, ka, B1, B2, ldb, kb, co, Out, nc);
+}
+
+static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const float* X, const float* Wg, const float* Wu,
+                    const float* Wd, int act, float* Y, char* ws, hipStream_t s) {
+    float* H = reinterpret_cast<float*>(ws + L.h);
+    const int nf = (int)ceil_div(d.f, 64);
+    const bool sho = ffn_short(d.n, 128, nf);
+    auto* up = sho ? k_ffn_up_f32<2> : k_ffn_up_f32<4>;
+    hipLaunchKernelGGL(up, dim3((unsigned)(ceil_div(d.n, sho ? 64 : 128) * nf)), dim3(kFfnThreads), 0, s, X, d.n, d.ci, Wg,
+                       Wu, d.f, act, H, d.f8, nf);
+    ffn_gemm_f32<false>(H, nullptr, d.f8, d.n, d.f8, Wd, nullptr, d.co, d.f, d.co, Y, s);
+}
+
+static void ffn_bwd_rows(const FfnShape& d, const FfnLayout& L, const float* X, const float* Wg, const float* Wu,
+                         const float* Wd, const float* dY, int act, float* dX, char* ws, hipStream_t s) {
+    float* H = reinterpret_cast<float*>(ws + L.h);
+    float* dGU = reinterpret_cast<float*>(ws + L.dgu);
+    const int nf = (int)ceil_div(d.f, 64);
+    const bool sho = ffn_short(d.n, 128, nf);
+    auto* mid = sho ? k_ffn_mid_f32<2> : k_ffn_mid_f32<4>;
+    hipLaunchKernelGGL(mid, dim3((unsigned)(ceil_div(d.n, sho ? 64 : 128) * nf)), dim3(kFfnThreads), 0, s, X, dY, d.n,
+                       d.ci, d.co, Wg, Wu, Wd, d.f, act, H, dGU, (int)d.f8, nf);
+    if (dX) ffn_gemm_f32<true>(dGU, dGU + d.f8, 2 * d.f8, d.n, d.f8, Wg, Wu, d.f, d.f, d.ci, dX, s);
+}
+
+static void ffn_dw(const FfnLayout& L, const DwSide<float>& p0, const DwSide<float>& p1, int64_t n, float* part,
+                   hipStream_t s) {
+    auto* kern = L.m_nar ? (L.n_nar ? k_ffn_dw_f32<2, 2> : k_ffn_dw_f32<2, 4>)
+                         : (L.n_nar ? k_ffn_dw_f32<4, 2> : k_ffn_dw_f32<4, 4>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(L.chunks * (p0.tiles + p1.tiles))), dim3(kFfnThreads), 0, s, p0, p1, n,
+                       L.chunk, L.per_chunk, part);
+}
+
+// --- bfloat16
+// A matrix as the tiles take it: itself, or (whole) a padded copy that `pad` is to make.
+struct FfnMat {
+    const uint16_t* p;
+    int64_t ld;
+};
+static FfnMat ffn_mat(const uint16_t* p, int64_t rows, int cols, char* copy, FfnPad& pad) {
+    if (cols % 8 == 0 && reinterpret_cast<uintptr_t>(p) % 16 == 0) return {p, cols};
+    const int i = pad.count++;
+    pad.src[i] = p;
+    pad.dst[i] = reinterpret_cast<uint16_t*>(copy);
+    pad.cols[i] = cols;
+    pad.ld[i] = (int)pad8(cols);
+    pad.end[i] = (i ? pad.end[i - 1] : 0) + rows * (pad.ld[i] / 8);
+    return {pad.dst[i], pad.ld[i]};
+}
+static void ffn_pad(const FfnPad& pad, hipStream_t s) {
+    if (pad.count == 0) return;
+    const int64_t blocks = ceil_div(pad.end[pad.count - 1], kFfnThreads);
+    hipLaunchKernelGGL(k_ffn_pad, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kFfnThreads), 0, s, pad);
+}
+
+template <FbB BK>
+static void ffn_gemm_bf16(const uint16_t* A1, const uint16_t* A2, int64_t lda, int64_t n, int64_t k, const uint16_t* B1,
+                          const uint16_t* B2, int64_t ldb, int co, uint16_t* Out, hipStream_t s) {
+    const bool nar = co <= 64;
+    const int nc = (int)ceil_div(co, nar ? 64 : 128);
+    const bool sho = !nar && ffn_short(n, 256, nc);
+    auto* kern = nar ? k_ffn_gemm_bf16<4, 1, 4, BK> : (sho ? k_ffn_gemm_bf16<2, 2, 4, BK> : k_ffn_gemm_bf16<2, 2, 8, BK>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(n, sho ? 128 : 256) * nc)), dim3(256), 0, s, A1, A2, lda, n, k, B1,
+                       B2, ldb, co, Out, nc);
+}
+
+static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const uint16_t* X, const uint16_t* Wg, const uint16_t* Wu,
+                    const uint16_t* Wd, int act, uint16_t* Y, char* ws, hipStream_t s) {
+    uint16_t* H = reinterpret_cast<uint16_t*>(ws + L.h);
+    FfnPad pad{};
+    const FfnMat x = ffn_mat(X, d.n, d.ci, ws + L.x, pad), g = ffn_mat(Wg, d.ci, d.f, ws + L.wg, pad),
+                 u = ffn_mat(Wu, d.ci, d.f, ws + L.wu, pad), w = ffn_mat(Wd, d.f, d.co, ws + L.wd, pad);
+    ffn_pad(pad, s);
+    const int nf = (int)ceil_div(d.f, 64);
+    const bool sho = ffn_short(d.n, 256, nf);
+    auto* up = sho ? k_ffn_up_bf16<4> : k_ffn_up_bf16<8>;
+    hipLaunchKernelGGL(up, dim3((unsigned)(ceil_div(d.n, sho ? 128 : 256) * nf)), dim3(256), 0, s, x.p, x.ld, d.n, d.ci,
+                       g.p, u.p, g.ld, d.f, act, H, d.f8, nf);
+    ffn_gemm_bf16<FB_MC>(H, nullptr, d.f8, d.n, d.f, w.p, nullptr, w.ld, d.co, Y, s);
+}
+
+static void ffn_dw(const FfnLayout& L, const DwSide<uint16_t>& p0, const DwSide<uint16_t>& p1, int64_t n, float* part,
+                   hipStream_t s) {
+    auto* kern = L.m_nar ? (L.n_nar ? k_ffn_dw_bf16<4, true> : k_ffn_dw_bf16<4, false>)
+                         : (L.n_nar ? k_ffn_dw_bf16<8, true> : k_ffn_dw_bf16<8, false>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(L.chunks * (p0.tiles + p1.tiles))), dim3(256), 0, s, p0, p1, n, L.chunk,
+                       L.per_chunk, part);
+}
+
+// --- either type
+// A few rows: H in float32.
 template <typename T>
-static void ffn_bwd(const FfnBwdLayout& L, const T* X, int64_t n, int ci, const T* Wg, const T* Wu, int f, const T* Wd,
-                    int co, const T* dY, int act, T* dX, T* dWg, T* dWu, T* dWd, char* ws, hipStream_t s) {
+static void ffn_fwd_few(const FfnShape& d, const FfnLayout& L, const T* X, const T* Wg, const T* Wu, const T* Wd, int act,
+                        T* Y, char* ws, hipStream_t s) {
+    constexpr int W = kFewCols * (16 / (int)sizeof(T));
+    float* H = reinterpret_cast<float*>(ws + L.h);
+    const int n = (int)d.n;
+    auto* up = n == 1 ? k_ffn_few<T, T, float, 1, true> : (n == 2 ? k_ffn_few<T, T, float, 2, true> : k_ffn_few<T, T, float, 4, true>);
+    auto* down = n == 1 ? k_ffn_few<float, T, T, 1, false>
+                        : (n == 2 ? k_ffn_few<float, T, T, 2, false> : k_ffn_few<float, T, T, 4, false>);
+    hipLaunchKernelGGL(up, dim3((unsigned)ceil_div(d.f, W)), dim3(kFfnThreads), 0, s, X, (int64_t)d.ci, n, d.ci, Wg, Wu,
+                       d.f, act, H, d.f8);
+    hipLaunchKernelGGL(down, dim3((unsigned)ceil_div(d.co, W)), dim3(kFfnThreads), 0, s, (const float*)H, d.f8, n, d.f, Wd,
+                       (const T*)nullptr, d.co, act, Y, (int64_t)d.co);
+}
+
+template <typename T>
+static void ffn_bwd(const FfnShape& d, const FfnLayout& L, const T* X, const T* Wg, const T* Wu, const T* Wd, const T* dY,
+                    int act, T* dX, T* dWg, T* dWu, T* dWd, char* ws, hipStream_t s) {
+    const int64_t n = d.n;
     T* H = reinterpret_cast<T*>(ws + L.h);
     T* dGU = reinterpret_cast<T*>(ws + L.dgu);
     float* part = reinterpret_cast<float*>(ws + L.part);
+    const T *xs = X, *ys = dY;
+    int64_t ldx = d.ci, ldy = d.co;
     if (n > 0) {
-        const int nf = (int)ceil_div(f, 64);
-        const bool sho = ffn_short(n, nf);
-        auto* mid = sho ? k_ffn_mid<T, 2> : k_ffn_mid<T, 4>;
-        hipLaunchKernelGGL(mid, dim3((unsigned)(ceil_div(n, sho ? 64 : 128) * nf)), dim3(kFfnThreads), 0, s, X, dY, n, ci, co, Wg, Wu, Wd, f, act, H, dGU, (int)L.f8, nf);
-        if (dX) ffn_gemm<T, true>(dGU, dGU + L.f8, 2 * L.f8, n, L.f8, Wg, Wu, f, f, ci, dX, s);
+        if constexpr (sizeof(T) == 2) {
+            FfnPad pad{};
+            const FfnMat x = ffn_mat(X, n, d.ci, ws + L.x, pad), y = ffn_mat(dY, n, d.co, ws + L.dy, pad),
+                         g = ffn_mat(Wg, d.ci, d.f, ws + L.wg, pad), u = ffn_mat(Wu, d.ci, d.f, ws + L.wu, pad),
+                         w = ffn_mat(Wd, d.f, d.co, ws + L.wd, pad);
+            ffn_pad(pad, s);
+            xs = x.p;
+            ys = y.p;
+            ldx = x.ld;
+            ldy = y.ld;
+            const int nf = (int)ceil_div(d.f, 64);
+            hipLaunchKernelGGL(k_ffn_mid_bf16<4>, dim3((unsigned)(ceil_div(n, 128) * nf)), dim3(256), 0, s, x.p, x.ld, y.p,
+                               y.ld, n, d.ci, d.co, g.p, u.p, g.ld, w.p, w.ld, d.f, act, H, dGU, (int)d.f8, nf);
+            if (dX) ffn_gemm_bf16<FB_KC>(dGU, dGU + d.f8, 2 * d.f8, n, d.f, g.p, u.p, g.ld, d.ci, dX, s);
+        } else {
+            ffn_bwd_rows(d, L, X, Wg, Wu, Wd, dY, act, dX, ws, s);
+        }
     }
     if (!dWg && !dWu && !dWd) return;
     const bool up = dWg || dWu;
-    DwSide<T> p0{X, dGU, ci, 2 * L.f8, ci, (int)(2 * L.f8), L.tn0, up ? L.t0 : 0, 0};
-    DwSide<T> p1{H, dY, L.f8, co, f, co, L.tn1, dWd ? L.t1 : 0, L.up};
-    const int64_t chunks = n > 0 ? L.chunks : 0;
-    if (n > 0) {
-        auto* kern = L.m_nar ? (L.n_nar ? k_ffn_dw<T, 2, 2> : k_ffn_dw<T, 2, 4>)
-                             : (L.n_nar ? k_ffn_dw<T, 4, 2> : k_ffn_dw<T, 4, 4>);
-        hipLaunchKernelGGL(kern, dim3((unsigned)(chunks * (p0.tiles + p1.tiles))), dim3(kFfnThreads), 0, s, p0, p1, n,
-                           L.chunk, L.per_chunk, part);
-    }
+    const DwSide<T> p0{xs, dGU, ldx, 2 * d.f8, d.ci, (int)(2 * d.f8), L.tn0, up ? L.t0 : 0, 0};
+    const DwSide<T> p1{H, ys, d.f8, ldy, d.f, d.co, L.tn1, dWd ? L.t1 : 0, L.up};
+    if (n > 0) ffn_dw(L, p0, p1, n, part, s);
     const int64_t total = dWd ? L.per_chunk : L.up;
     const int64_t blocks = ceil_div(total, kFfnThreads);
     hipLaunchKernelGGL(k_ffn_dw_sum<T>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kFfnThreads), 0, s, part,
-                       chunks, L.per_chunk, ci, f, (int)L.f8, co, dWg, dWu, dWd, L.up, total);
+                       n > 0 ? L.chunks : 0, L.per_chunk, d.ci, d.f, (int)d.f8, d.co, dWg, dWu, dWd, L.up, total);
 }
 
 }  // namespace gsc
@@ -721,7 +763,7 @@ extern "C" {
 
 size_t gsc_gated_ffn_fwd_ws_bytes(int32_t dtype, int64_t n, int32_t c_in, int32_t hidden, int32_t c_out) {
     if (!ffn_sizes_ok(dtype, n, c_in, hidden, c_out)) return 0;
-    return ffn_al256((size_t)n * pad8(hidden) * ffn_size(dtype));
+    return ffn_layout(dtype, FfnShape(n, c_in, hidden, c_out), false).total;
 }
 
 int gsc_gated_ffn_fwd(int32_t dtype, const void* X, int64_t n, int32_t c_in, const void* Wg, const void* Wu,
@@ -737,24 +779,27 @@ int gsc_gated_ffn_fwd(int32_t dtype, const void* X, int64_t n, int32_t c_in, con
         return fail(GSC_EINVAL, "gated_ffn_fwd: more tiles than a launch takes");
     if (n == 0) return GSC_OK;
     if (!X || !Wg || !Wu || !Wd || !Y) return fail(GSC_EINVAL, "gated_ffn_fwd: null X/Wg/Wu/Wd/Y");
-    const size_t need = gsc_gated_ffn_fwd_ws_bytes(dtype, n, c_in, hidden, c_out);
-    if (!ws || ws_bytes < need)
-        return fail(GSC_ESHORT, "gated_ffn_fwd: ws needs %zu bytes, got %zu", need, ws ? ws_bytes : (size_t)0);
+    const FfnShape d(n, c_in, hidden, c_out);
+    const FfnLayout L = ffn_layout(dtype, d, false);
+    if (!ws || ws_bytes < L.total)
+        return fail(GSC_ESHORT, "gated_ffn_fwd: ws needs %zu bytes, got %zu", L.total, ws ? ws_bytes : (size_t)0);
     if (reinterpret_cast<uintptr_t>(ws) % 16) return fail(GSC_EINVAL, "gated_ffn_fwd: ws must be aligned to 16 bytes");
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (dtype == GSC_BF16)
-        ffn_fwd<uint16_t>((const uint16_t*)X, n, c_in, (const uint16_t*)Wg, (const uint16_t*)Wu, hidden,
-                          (const uint16_t*)Wd, c_out, act, (uint16_t*)Y, (uint16_t*)ws, s);
-    else
-        ffn_fwd<float>((const float*)X, n, c_in, (const float*)Wg, (const float*)Wu, hidden, (const float*)Wd, c_out,
-                       act, (float*)Y, (float*)ws, s);
+    auto run = [&](auto t) {
+        typedef decltype(t) T;
+        const T *x = (const T*)X, *g = (const T*)Wg, *u = (const T*)Wu, *w = (const T*)Wd;
+        if (n <= kFfnFewRows) ffn_fwd_few<T>(d, L, x, g, u, w, act, (T*)Y, (char*)ws, s);
+        else ffn_fwd(d, L, x, g, u, w, act, (T*)Y, (char*)ws, s);
+    };
+    if (dtype == GSC_BF16) run(uint16_t{});
+    else run(float{});
     GSC_LAUNCH_CHECK();
     return GSC_OK;
 }
 
 size_t gsc_gated_ffn_bwd_ws_bytes(int32_t dtype, int64_t n, int32_t c_in, int32_t hidden, int32_t c_out) {
     if (!ffn_sizes_ok(dtype, n, c_in, hidden, c_out)) return 0;
-    return ffn_bwd_layout(dtype, n, c_in, hidden, c_out).total;
+    return ffn_layout(dtype, FfnShape(n, c_in, hidden, c_out), true).total;
 }
 
 int gsc_gated_ffn_bwd(int32_t dtype, const void* X, int64_t n, int32_t c_in, const void* Wg, const void* Wu,
@@ -772,18 +817,19 @@ int gsc_gated_ffn_bwd(int32_t dtype, const void* X, int64_t n, int32_t c_in, con
     if (!dX && !dWg && !dWu && !dWd) return GSC_OK;
     if (n == 0 && !dWg && !dWu && !dWd) return GSC_OK;
     if (n > 0 && (!X || !Wg || !Wu || !Wd || !dY)) return fail(GSC_EINVAL, "gated_ffn_bwd: null X/Wg/Wu/Wd/dY");
-    const FfnBwdLayout L = ffn_bwd_layout(dtype, n, c_in, hidden, c_out);
+    const FfnShape d(n, c_in, hidden, c_out);
+    const FfnLayout L = ffn_layout(dtype, d, true);
     if (!ws || ws_bytes < L.total)
         return fail(GSC_ESHORT, "gated_ffn_bwd: ws needs %zu bytes, got %zu", L.total, ws ? ws_bytes : (size_t)0);
     if (reinterpret_cast<uintptr_t>(ws) % 16) return fail(GSC_EINVAL, "gated_ffn_bwd: ws must be aligned to 16 bytes");
     hipStream_t s = reinterpret_cast<hipStream_t>(stream);
-    if (dtype == GSC_BF16)
-        ffn_bwd<uint16_t>(L, (const uint16_t*)X, n, c_in, (const uint16_t*)Wg, (const uint16_t*)Wu, hidden,
-                          (const uint16_t*)Wd, c_out, (const uint16_t*)dY, act, (uint16_t*)dX, (uint16_t*)dWg,
-                          (uint16_t*)dWu, (uint16_t*)dWd, (char*)ws, s);
-    else
-        ffn_bwd<float>(L, (const float*)X, n, c_in, (const float*)Wg, (const float*)Wu, hidden, (const float*)Wd, c_out,
-                       (const float*)dY, act, (float*)dX, (float*)dWg, (float*)dWu, (float*)dWd, (char*)ws, s);
+    auto run = [&](auto t) {
+        typedef decltype(t) T;
+        ffn_bwd<T>(d, L, (const T*)X, (const T*)Wg, (const T*)Wu, (const T*)Wd, (const T*)dY, act, (T*)dX, (T*)dWg,
+                   (T*)dWu, (T*)dWd, (char*)ws, s);
+    };
+    if (dtype == GSC_BF16) run(uint16_t{});
+    else run(float{});
     GSC_LAUNCH_CHECK();
     return GSC_OK;
 }

@@ -1,0 +1,192 @@
+// Tile product of float32 operands for the feed-forward block (ffn.hip): 32 MT x 32 NT outputs per block of
+// four waves on v_mfma_f32_16x16x4f32, the operands' next 128 bytes of the reduction in registers
+// while the current ones are read from LDS (two stages, one barrier a step).  An operand lies either with the
+// reduction along its rows (KC) or across them (MC) and is copied to LDS as it lies; operands
+// may start at any float.
+#pragma once
+
+#include "row_vec.h"
+
+namespace gsc {
+
+constexpr int kFfnThreads = 256;
+constexpr int kFfnRowBytes = 128;               // reduction bytes of a step
+constexpr int kFfnBk = kFfnRowBytes / 4;
+
+// One side of a product: `rows` outputs by k reduction elements, element (r, k) at p[r ld + k] (KC)
+// or p[k ld + r] (MC).  Rows and reduction elements behind the end read as 0.  SPLIT: the tile's rows
+// [0, R / 2) come from p and the others from p2 (both from row 0 on).
+struct Side {
+    const float* p;
+    const float* p2;
+    int64_t ld;
+    int64_t rows;
+    int64_t k;
+};
+
+// A thread's share of a tile of R rows by one step, through registers into LDS.
+template <bool KC, int R, bool SPLIT>
+struct TileCopy {
+    static constexpr int V = 4, BK = kFfnBk;
+    static constexpr int N = R * kFfnRowBytes / 16 / kFfnThreads;   // 16-byte pieces a thread
+    static constexpr int PER = KC ? BK / V : R / V;                 // pieces of a row (KC) or of a reduction element
+    static_assert(N >= 1 && kFfnThreads % PER == 0, "tile");
+    typedef RowVec<float>::Raw Raw;
+
+    const float* base;      // element (0, 0) of the thread's side
+    int64_t ld;
+    int line, at;       // first row (KC) or reduction element (MC), and the piece's first element across
+    int64_t across;     // MC: elements from `at` to the rows' end
+    int lim;            // KC: valid lines
+    Raw r[N];
+
+    __device__ __forceinline__ void start(const Side& s) {
+        const int c = threadIdx.x % PER;
+        line = threadIdx.x / PER;
+        at = c * V;
+        base = s.p;
+        ld = s.ld;
+        if (KC) {
+            lim = (int)(s.rows < R ? s.rows : R);
+            across = 0;
+        } else {
+            int col = at;
+            if (SPLIT && at >= R / 2) {
+                base = s.p2;
+                col -= R / 2;
+            }
+            across = s.rows - col;
+            if (SPLIT && across > R / 2 - col) across = R / 2 - col;
+            base += col;
+            lim = 0;
+        }
+    }
+    // the step at reduction element k0
+    __device__ __forceinline__ void fetch(int64_t k0, int64_t k) {
+        constexpr int DL = kFfnThreads / PER;   // lines between a thread's pieces
+        if (KC) {
+            const float* b = base + k0 + at;
+            const int64_t left = k - k0 - at;
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int row = line + j * DL;
+                r[j] = load_vec<float, true>(b + (int64_t)row * ld, row < lim ? left : 0);
+            }
+        } else {
+            const float* b = base + k0 * ld;
+            const int kl = (int)(k - k0 < BK ? k - k0 : BK);
+#pragma unroll
+            for (int j = 0; j < N; ++j) {
+                const int kk = line + j * DL;
+                r[j] = load_vec<float, true>(b + (int64_t)kk * ld, kk < kl ? across : 0);
+            }
+        }
+    }
+    __device__ __forceinline__ void put(uint8_t* lds) const {
+        constexpr int DL = kFfnThreads / PER;
+        const int c = threadIdx.x % PER;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const int row = line + j * DL;
+            *reinterpret_cast<uint4*>(lds + place(row, c)) = uint4{r[j][0], r[j][1], r[j][2], r[j][3]};
+        }
+    }
+    // Byte of piece c of a line.  KC: lines of 128 bytes, pieces permuted by the row modulo 8, so the
+    // eight rows that a read serves together lie in distinct banks.  MC: 64-byte groups permuted by bits 2 and
+    // 3 of the reduction element (a lane's q).
+    static __device__ __forceinline__ int place(int row, int c) {
+        if (KC) return row * kFfnRowBytes + ((c ^ (row & 7)) * 16);
+        constexpr int M = PER / 4 - 1;
+        return row * (R * 4) + (((c >> 2) ^ ((row >> 2) & 3 & M)) * 64) + (c & 3) * 16;
+    }
+};
+
+// Fragment reads of one wave: operand of 16 rows from row0, reduction elements of group kk (16 of the
+// step's 32); lane (i, q) holds row i, elements 4 q .. 4 q + 3, and MFMA s of the four takes the s-th of
+// each (the sum does not care which four elements a product takes together).
+template <bool KC, int R>
+struct Frag {
+    typedef floatx4 Reg;
+    static __device__ __forceinline__ Reg read(const uint8_t* lds, int row0, int kk) {
+        const int lane = threadIdx.x & 63, i = lane & 15, q = lane >> 4;
+        if constexpr (KC) {
+            const int row = row0 + i;
+            return *reinterpret_cast<const floatx4*>(lds + row * kFfnRowBytes + (((kk * 4 + q) ^ (row & 7)) * 16));
+        } else {
+            constexpr int M = R / 16 - 1;
+            floatx4 v;
+#pragma unroll
+            for (int s = 0; s < 4; ++s) {
+                const int k = kk * 16 + 4 * q + s;
+                v[s] = *reinterpret_cast<const float*>(lds + k * (R * 4) + (((row0 >> 4) ^ (q & M)) * 64) + i * 4);
+            }
+            return v;
+        }
+    }
+};
+
+// LDS of a block: two stages of both operands.
+template <int MT, int NT>
+constexpr int ffn_lds() { return 2 * 32 * (MT + NT) * kFfnRowBytes; }
+
+// acc[mi][ni] += the tile's product.  Four waves, (wm, wn) = 2 x 2: wave rows 16 MT wm .., columns
+// 16 NT wn .. (SPLIT: half of them from either half of the tile's columns).  The second operand goes
+// into the MFMA first, so lane (i, q) gets row 16 mi + i of its rows and four consecutive columns 4 q ..
+// of block ni.  LDS may be in use by other waves' earlier reads: starts with a barrier.
+template <bool AKC, bool BKC, int MT, int NT, bool SPLIT>
+__device__ __forceinline__ void tile_product(const Side& A, const Side& B, uint8_t* lds, floatx4 (&acc)[MT][NT]) {
+    constexpr int RA = 32 * MT, RB = 32 * NT, BK = kFfnBk;
+    constexpr int STAGE = (RA + RB) * kFfnRowBytes;
+    typedef Frag<AKC, RA> FA;
+    typedef Frag<BKC, RB> FB;
+    TileCopy<AKC, RA, false> ca;
+    TileCopy<BKC, RB, SPLIT> cb;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+    const int64_t K = A.k;
+    ca.start(A);
+    cb.start(B);
+    ca.fetch(0, K);
+    cb.fetch(0, B.k);
+    __syncthreads();
+    ca.put(lds);
+    cb.put(lds + RA * kFfnRowBytes);
+    __syncthreads();
+    int cur = 0;
+    for (int64_t k0 = 0; k0 < K; k0 += BK) {
+        const bool more = k0 + BK < K;
+        if (more) {
+            ca.fetch(k0 + BK, K);
+            cb.fetch(k0 + BK, B.k);
+        }
+        const uint8_t* la = lds + cur * STAGE;
+        const uint8_t* lb = la + RA * kFfnRowBytes;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+            typename FA::Reg a[MT], b[NT];
+#pragma unroll
+            for (int mi = 0; mi < MT; ++mi) a[mi] = FA::read(la, 16 * (MT * wm + mi), kk);
+#pragma unroll
+            for (int ni = 0; ni < NT; ++ni) {
+                const int col = !SPLIT ? 16 * (NT * wn + ni)
+                                       : 16 * (NT / 2 * wn + ni % (NT / 2)) + (ni < NT / 2 ? 0 : RB / 2);
+                b[ni] = FB::read(lb, col, kk);
+            }
+#pragma unroll
+            for (int s = 0; s < 4; ++s)   // (the products of one sum are MT NT instructions apart)
+#pragma unroll
+                for (int mi = 0; mi < MT; ++mi)
+#pragma unroll
+                    for (int ni = 0; ni < NT; ++ni)
+                        acc[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x4f32(b[ni][s], a[mi][s], acc[mi][ni], 0, 0, 0);
+        }
+        if (more) {
+            cur ^= 1;
+            uint8_t* ld = lds + cur * STAGE;
+            ca.put(ld);
+            cb.put(ld + RA * kFfnRowBytes);
+        }
+        __syncthreads();
+    }
+}
+
+}  // namespace gsc
