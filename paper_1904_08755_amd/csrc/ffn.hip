@@ -83,24 +83,38 @@ __device__ __forceinline__ void with_act(int act, F f) {
     }
 }
 
-// four consecutive columns of a row
-__device__ __forceinline__ void store4(float* p, int64_t left, const float (&v)[4]) {
-    if (left >= 4) {
-        *reinterpret_cast<floatx4u*>(p) = floatx4u{v[0], v[1], v[2], v[3]};
-    } else {
+// Four consecutive columns of a row from each of two neighbouring 16-column blocks, as a lane holds them (columns col ..
+// and col + 16 .., col = 32 c + 4 q), stored below `limit` to the row at p.  bfloat16: lanes q and q + 1 exchange
+// halves (permlane16_swap) so that each has 16 bytes of one block: a store of 64 lanes covers 16 rows by
+// 64 bytes.  (8 bytes a lane in 32-byte pieces: k_ffn_mid spent as long storing as on everything else.)
+__device__ __forceinline__ void store_pair(float* p, int64_t col, int64_t limit, bool on, const float (&u)[4],
+                                           const float (&v)[4]) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) p[e] = v[e];
+    for (int b = 0; b < 2; ++b) {
+        const float (&w)[4] = b ? v : u;
+        const int64_t at = col + 16 * b;
+        if (on && at + 4 <= limit) {
+            *reinterpret_cast<floatx4u*>(p + at) = floatx4u{w[0], w[1], w[2], w[3]};
+        } else if (on) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (at + e < limit) p[at + e] = w[e];
+        }
     }
 }
-__device__ __forceinline__ void store4(uint16_t* p, int64_t left, const float (&v)[4]) {
-    typedef uint32_t u32x2u __attribute__((ext_vector_type(2), aligned(2)));
-    if (left >= 4) {
-        *reinterpret_cast<u32x2u*>(p) = u32x2u{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
-    } else {
+__device__ __forceinline__ void store_pair(uint16_t* p, int64_t col, int64_t limit, bool on, const float (&u)[4],
+                                           const float (&v)[4]) {
+    const int q = (threadIdx.x & 63) >> 4;
+    const auto lo = __builtin_amdgcn_permlane16_swap(pack_bf16(u[0], u[1]), pack_bf16(v[0], v[1]), false, false);
+    const auto hi = __builtin_amdgcn_permlane16_swap(pack_bf16(u[2], u[3]), pack_bf16(v[2], v[3]), false, false);
+    const RowVec<uint16_t>::Raw w = {lo[0], hi[0], lo[1], hi[1]};
+    const int64_t at = col - 4 * q + 16 * (q & 1) + 8 * (q >> 1);
+    if (on && at + 8 <= limit) {
+        *reinterpret_cast<RowVec<uint16_t>::Raw*>(p + at) = w;
+    } else if (on) {
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if (e < left) store_out(&p[e], v[e]);
+        for (int e = 0; e < 8; ++e)
+            if (at + e < limit) p[at + e] = (uint16_t)(w[e >> 1] >> (16 * (e & 1)));
     }
 }
 
@@ -126,12 +140,11 @@ __device__ __forceinline__ void store_tile(const floatx4 (&acc)[MT][NT], int64_t
 #pragma unroll
     for (int mi = 0; mi < MT; ++mi) {
         const int64_t row = row0 + 16 * mi + ffn_i();
-        if (row >= n) continue;
 #pragma unroll
-        for (int ni = 0; ni < NT; ++ni) {
-            const int64_t col = col0 + 16 * ni + 4 * ffn_q();
-            const float v[4] = {acc[mi][ni][0], acc[mi][ni][1], acc[mi][ni][2], acc[mi][ni][3]};
-            if (col < nn) store4(out + row * ld + col, nn - col, v);
+        for (int ni = 0; ni < NT; ni += 2) {
+            const float u[4] = {acc[mi][ni][0], acc[mi][ni][1], acc[mi][ni][2], acc[mi][ni][3]};
+            const float v[4] = {acc[mi][ni + 1][0], acc[mi][ni + 1][1], acc[mi][ni + 1][2], acc[mi][ni + 1][3]};
+            store_pair(out + row * ld, col0 + 16 * ni + 4 * ffn_q(), nn, row < n, u, v);
         }
     }
 }
@@ -144,19 +157,16 @@ __device__ __forceinline__ void store_hidden(const floatx4 (&acc)[MT][4], int64_
 #pragma unroll
         for (int mi = 0; mi < MT; ++mi) {
             const int64_t row = row0 + 16 * mi + ffn_i();
-            if (row >= n) continue;
+            float h[2][4];
 #pragma unroll
-            for (int ni = 0; ni < 2; ++ni) {
-                const int64_t col = col0 + 16 * ni + 4 * ffn_q();
-                float h[4];
+            for (int ni = 0; ni < 2; ++ni)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float a, d;
                     ffn_act<decltype(ACT)::value, false>(acc[mi][ni][e], a, d);
-                    h[e] = a * acc[mi][ni + 2][e];
+                    h[ni][e] = a * acc[mi][ni + 2][e];
                 }
-                store4(H + row * ldh + col, ldh - col, h);
-            }
+            store_pair(H + row * ldh, col0 + 4 * ffn_q(), ldh, row < n, h[0], h[1]);
         }
     });
 }
@@ -170,24 +180,22 @@ __device__ __forceinline__ void store_mid(const floatx4 (&acc)[MT][4], const flo
 #pragma unroll
         for (int mi = 0; mi < MT; ++mi) {
             const int64_t row = row0 + 16 * mi + ffn_i();
-            if (row >= n) continue;
+            float h[2][4], dg[2][4], du[2][4];
 #pragma unroll
-            for (int ni = 0; ni < 2; ++ni) {
-                const int64_t col = col0 + 16 * ni + 4 * ffn_q();
-                float h[4], dg[4], du[4];
+            for (int ni = 0; ni < 2; ++ni)
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float a, d;
                     ffn_act<decltype(ACT)::value, true>(acc[mi][ni][e], a, d);
                     const float up = acc[mi][ni + 2][e], g = dh[mi][ni][e];
-                    h[e] = a * up;
-                    dg[e] = g * up * d;
-                    du[e] = g * a;
+                    h[ni][e] = a * up;
+                    dg[ni][e] = g * up * d;
+                    du[ni][e] = g * a;
                 }
-                store4(H + row * f8 + col, f8 - col, h);
-                store4(dGU + row * 2 * f8 + col, f8 - col, dg);
-                store4(dGU + row * 2 * f8 + f8 + col, f8 - col, du);
-            }
+            const int64_t col = col0 + 4 * ffn_q();
+            store_pair(H + row * f8, col, f8, row < n, h[0], h[1]);
+            store_pair(dGU + row * 2 * f8, col, f8, row < n, dg[0], dg[1]);
+            store_pair(dGU + row * 2 * f8 + f8, col, f8, row < n, du[0], du[1]);
         }
     });
 }
@@ -540,10 +548,11 @@ struct FfnLayout {
 // float32: tiles of 64 outputs instead of 128 in a direction where they leave less of the last one empty.
 static bool ffn_narrow(int64_t rows) { return ceil_div(rows, 64) % 2 == 1 && rows < 512; }
 
-// Row chunks of the weights' gradients: about four blocks a compute unit, at least 512 rows each.
+// Row chunks of the weights' gradients: as many as fill the device once with two blocks a compute unit (a few blocks more
+// would take a second round: 1,032 blocks 605 us, 504 blocks 525 us), at least 512 rows each.
 constexpr int64_t kFfnChunkRows = 512;
 static int64_t ffn_chunks(int64_t n, int64_t tiles) {
-    int64_t c = ceil_div(4 * 256, tiles);
+    int64_t c = 512 / tiles;
     const int64_t most = ceil_div(n, kFfnChunkRows);
     if (c > most) c = most;
     return c < 1 ? 1 : c;

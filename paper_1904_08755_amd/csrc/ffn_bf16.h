@@ -28,7 +28,6 @@ typedef short fs16x4 __attribute__((ext_vector_type(4)));
 
 constexpr int kFbBufFlags = 0x00020000;       // buffer descriptor word 3: 32-bit data format
 constexpr uint32_t kFbNone = 0x80000000u;     // an offset past any operand's end
-constexpr int kFbStages = 3;
 
 // s_waitcnt operand: vmcnt(n), the other counters left free (gfx9 encoding)
 template <int N>
@@ -221,15 +220,15 @@ enum FbB { FB_KC, FB_MC, FB_PAIR };
 
 // acc += A B^T of a block of WM x WN waves, wave tiles of 16 MT rows by 16 NT columns.  The second operand
 // goes into the MFMA first: lane (i, q) gets row 16 mi + i of its rows and four consecutive columns
-// 4 q .. of block ni.  lds: kFbStages stages of fb_stage bytes.  Every wave has passed its last read of lds before the call.
-template <int WM, int WN, int MT, int NT>
+// 4 q .. of block ni.  lds: NS stages.  Every wave has passed its last read of lds before the call.
+template <int WM, int WN, int MT, int NT, int NS = 3>
 struct FbShape {
     static constexpr int NW = WM * WN, BM = 16 * MT * WM, BN = 16 * NT * WN;
     static constexpr int STAGE = (BM + BN) * 64;
-    static constexpr int LDS = kFbStages * STAGE;
+    static constexpr int LDS = NS * STAGE;
 };
 
-template <int WM, int WN, int MT, int NT, bool AMC, FbB BK>
+template <int WM, int WN, int MT, int NT, bool AMC, FbB BK, int NS = 3>
 __device__ __forceinline__ void fb_product(const FbSide& A, const FbSide& B, const uint16_t* b2, int64_t K, uint8_t* lds,
                                            floatx4 (&acc)[MT][NT]) {
     typedef FbShape<WM, WN, MT, NT> S;
@@ -267,15 +266,16 @@ __device__ __forceinline__ void fb_product(const FbSide& A, const FbSide& B, con
         for (int t = 0; t < NT; ++t)
             fb[t] = fb_lds(lds) + CA::BYTES + (t < NT / 2 ? 0 : CB::BYTES) + fb_frag_mc<RB>(NT / 2 * wn + t % (NT / 2));
     }
-    issue(0, 0);
-    if (steps > 1) issue(1, 1);
+#pragma unroll
+    for (int s = 0; s < NS - 1; ++s)
+        if (s < steps) issue(s, s);
     int slot = 0;
     for (int s = 0; s < steps; ++s) {
-        if (s + 1 < steps) fb_wait<LD>();
+        if (s + NS - 2 < steps) fb_wait<LD * (NS - 2)>();
         else fb_wait<0>();
         fb_barrier();
-        const int into = slot == 0 ? 2 : slot - 1;   // the stage of step s - 1, for step s + 2
-        if (s + 2 < steps) issue(s + 2, into);
+        const int into = slot == 0 ? NS - 1 : slot - 1;   // the stage of step s - 1
+        if (s + NS - 1 < steps) issue(s + NS - 1, into);
         fbf16x8 a[MT], b[NT];
         const uint32_t at = (uint32_t)(slot * S::STAGE);
         if constexpr (BK == FB_KC) {
@@ -298,7 +298,7 @@ __device__ __forceinline__ void fb_product(const FbSide& A, const FbSide& B, con
 #pragma unroll
             for (int ni = 0; ni < NT; ++ni)
                 acc[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[ni], a[mi], acc[mi][ni], 0, 0, 0);
-        slot = slot == 2 ? 0 : slot + 1;
+        slot = slot == NS - 1 ? 0 : slot + 1;
     }
 }
 
