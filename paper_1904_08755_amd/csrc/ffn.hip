@@ -19,69 +19,15 @@
 // are copied into the workspace first, their rows padded with zeros (k_ffn_pad; the weights and at
 // most three passes over rows, against kernels that would load element by element).  float32 tiles
 // (ffn_f32.h) take any address.
+#include "ffn_act.h"
 #include "ffn_bf16.h"
 #include "ffn_f32.h"
+#include "ffn_res.h"
 
 namespace gsc {
 
 constexpr int kFfnMaxWidth = 1 << 20;
 constexpr int kFfnFewRows = 4;                          // rows up to which k_ffn_few runs
-
-// ---------------------------------------------------------------------------
-// activations
-// ---------------------------------------------------------------------------
-__device__ __forceinline__ float ffn_exp(float x) { return __builtin_amdgcn_exp2f(x * 1.44269504088896f); }
-__device__ __forceinline__ float ffn_sigmoid(float x) { return __builtin_amdgcn_rcpf(1.f + ffn_exp(-x)); }
-
-// act(g) and (D) its derivative.  The hardware's exponential and reciprocal: within about |g| + 2 units in
-// the last place of float32, far inside what the products' sums lose.
-template <int ACT, bool D>
-__device__ __forceinline__ void ffn_act(float g, float& a, float& d) {
-    if constexpr (ACT == GSC_GATE_RELU) {
-        a = g < 0.f ? 0.f : g;   // NaN passes through
-        if (D) d = g > 0.f ? 1.f : 0.f;
-    } else if constexpr (ACT == GSC_GATE_SIGMOID) {
-        a = ffn_sigmoid(g);
-        if (D) d = a * (1.f - a);
-    } else if constexpr (ACT == GSC_GATE_SILU) {
-        const float p = ffn_sigmoid(g);
-        a = g * p;
-        if (D) d = fmaf(a, 1.f - p, p);
-    } else if constexpr (ACT == GSC_GATE_GELU) {
-        // the normal distribution function from Abramowitz & Stegun 7.1.26 (absolute error of erf 1.5e-7),
-        // its density shared with the derivative
-        const float z = fabsf(g) * 0.70710678118655f;
-        const float e = ffn_exp(-0.5f * g * g);
-        const float t = __builtin_amdgcn_rcpf(fmaf(0.3275911f, z, 1.f));
-        float q = fmaf(1.061405429f, t, -1.453152027f);
-        q = fmaf(q, t, 1.421413741f);
-        q = fmaf(q, t, -0.284496736f);
-        q = fmaf(q, t, 0.254829592f);
-        q = 0.5f * q * t * e;              // the upper tail at |g|
-        const float p = g < 0.f ? q : 1.f - q;
-        a = g * p;
-        if (D) d = fmaf(g * 0.398942280401433f, e, p);
-    } else {
-        // 0.5 (1 + tanh(u)) = sigmoid(2 u)
-        const float k = 0.797884560802865f, c = 0.044715f;
-        const float g2 = g * g;
-        const float p = ffn_sigmoid(2.f * k * g * fmaf(c, g2, 1.f));
-        a = g * p;
-        if (D) d = fmaf(2.f * a * (1.f - p), k * fmaf(3.f * c, g2, 1.f), p);
-    }
-}
-
-// f(activation as a constant)
-template <typename F>
-__device__ __forceinline__ void with_act(int act, F f) {
-    switch (act) {
-        case GSC_GATE_RELU: f(std::integral_constant<int, GSC_GATE_RELU>{}); break;
-        case GSC_GATE_SIGMOID: f(std::integral_constant<int, GSC_GATE_SIGMOID>{}); break;
-        case GSC_GATE_GELU: f(std::integral_constant<int, GSC_GATE_GELU>{}); break;
-        case GSC_GATE_GELU_TANH: f(std::integral_constant<int, GSC_GATE_GELU_TANH>{}); break;
-        default: f(std::integral_constant<int, GSC_GATE_SILU>{}); break;
-    }
-}
 
 // Four consecutive columns of a row from each of two neighbouring 16-column blocks, as a lane holds them (columns col ..
 // and col + 16 .., col = 32 c + 4 q), stored below `limit` to the row at p.  bfloat16: lanes q and q + 1 exchange
@@ -536,14 +482,20 @@ struct FfnShape {
     FfnShape(int64_t n, int ci, int f, int co) : n(n), ci(ci), f(f), co(co), f8(pad8(f)) {}
 };
 
-// Workspace, in order: what the padded copies of X, dY (backward), Wg, Wu and Wd take (bfloat16), H, then for the
-// backward pass dG | dU and the weight gradients' partial sums.
+// Workspace, in order: what the padded copies of X, dY (backward), Wg, Wu and Wd and the packed weights take
+// (bfloat16), H, then for the backward pass dG | dU and the weight gradients' partial sums.
 struct FfnLayout {
-    size_t x, dy, wg, wu, wd, h, dgu, part, total;
+    size_t x, dy, wg, wu, wd, pack, h, dgu, part, total;
     int64_t per_chunk, up, chunks, chunk;
     bool m_nar, n_nar;      // tiles of 64 channels for the weight gradients of the first, of the second projection
     int tn0, t0, tn1, t1;
 };
+
+// Rows from which the kernels that keep rows in registers take them (bfloat16).
+constexpr int64_t kResFwdRows = 128 * 256, kResBwdRows = 128 * 64;
+static bool ffn_resident(const FfnShape& d, bool bwd) {
+    return d.ci <= kResMax && d.co <= kResMax && d.n >= (bwd ? kResBwdRows : kResFwdRows);
+}
 
 // float32: tiles of 64 outputs instead of 128 in a direction where they leave less of the last one empty.
 static bool ffn_narrow(int64_t rows) { return ceil_div(rows, 64) % 2 == 1 && rows < 512; }
@@ -574,6 +526,7 @@ static FfnLayout ffn_layout(int dtype, const FfnShape& d, bool bwd) {
         L.wg = take((size_t)d.ci * d.f8 * 2);
         L.wu = take((size_t)d.ci * d.f8 * 2);
         L.wd = take((size_t)d.f * pad8(d.co) * 2);
+        if (ffn_resident(d, bwd)) L.pack = take(res_pack_bytes(d.ci, d.f, d.co, bwd));
     }
     L.h = take((size_t)d.n * d.f8 * (d.n <= kFfnFewRows ? 4 : size));
     if (bwd) {
@@ -688,6 +641,10 @@ static void ffn_gemm_bf16(const uint16_t* A1, const uint16_t* A2, int64_t lda, i
 static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const uint16_t* X, const uint16_t* Wg, const uint16_t* Wu,
                     const uint16_t* Wd, int act, uint16_t* Y, char* ws, hipStream_t s) {
     uint16_t* H = reinterpret_cast<uint16_t*>(ws + L.h);
+    if (ffn_resident(d, false)) {
+        res_fwd(X, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, Y, ws + L.pack, s);
+        return;
+    }
     FfnPad pad{};
     const FfnMat x = ffn_mat(X, d.n, d.ci, ws + L.x, pad), g = ffn_mat(Wg, d.ci, d.f, ws + L.wg, pad),
                  u = ffn_mat(Wu, d.ci, d.f, ws + L.wu, pad), w = ffn_mat(Wd, d.f, d.co, ws + L.wd, pad);
@@ -746,8 +703,12 @@ static void ffn_bwd(const FfnShape& d, const FfnLayout& L, const T* X, const T* 
             ldx = x.ld;
             ldy = y.ld;
             const int nf = (int)ceil_div(d.f, 64);
-            hipLaunchKernelGGL(k_ffn_mid_bf16<4>, dim3((unsigned)(ceil_div(n, 128) * nf)), dim3(256), 0, s, x.p, x.ld, y.p,
-                               y.ld, n, d.ci, d.co, g.p, u.p, g.ld, w.p, w.ld, d.f, act, H, dGU, (int)d.f8, nf);
+            if (ffn_resident(d, true)) {
+                res_mid(X, dY, n, d.ci, Wg, Wu, d.f, Wd, d.co, act, H, dGU, d.f8, ws + L.pack, s);
+            } else {
+                hipLaunchKernelGGL(k_ffn_mid_bf16<4>, dim3((unsigned)(ceil_div(n, 128) * nf)), dim3(256), 0, s, x.p, x.ld,
+                                   y.p, y.ld, n, d.ci, d.co, g.p, u.p, g.ld, w.p, w.ld, d.f, act, H, dGU, (int)d.f8, nf);
+            }
             if (dX) ffn_gemm_bf16<FB_KC>(dGU, dGU + d.f8, 2 * d.f8, n, d.f, g.p, u.p, g.ld, d.ci, dX, s);
         } else {
             ffn_bwd_rows(d, L, X, Wg, Wu, Wd, dY, act, dX, ws, s);

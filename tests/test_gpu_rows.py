@@ -391,6 +391,26 @@ def test_gated_ffn_shapes(dtype, i):
     assert only[0] is None and all(torch.equal(p, q) for p, q in zip(only[1:], grads[1:]))
 
 
+# rows enough for the kernels that keep a block's rows in registers (bfloat16, up to 256 channels either side), and
+# widths beyond them
+FFN_MANY = [(8200, 40, 72, 24, 1), (9001, 256, 130, 200, 0), (16500, 128, 512, 128, 0), (33001, 64, 100, 64, 0),
+            (33333, 130, 267, 100, 1), (32769, 256, 64, 256, 0), (35000, 8, 40, 129, 0), (36011, 96, 200, 256, 0),
+            (40000, 200, 63, 8, 0), (34000, 257, 96, 64, 0), (33000, 33, 65, 1, 0)]
+
+
+@BOTH
+@pytest.mark.parametrize("i", range(len(FFN_MANY)))
+def test_gated_ffn_many_rows(dtype, i):
+    n, ci, f, co, at = FFN_MANY[i]
+    act = ACTS[i % len(ACTS)]
+    X, Wg, Wu, Wd, dY = _ffn_inputs(dtype, n, ci, f, co, at)
+    Y = gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd, act)
+    grads = gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, act)
+    _ffn_check(X, Wg, Wu, Wd, dY, act, Y, grads)
+    assert torch.equal(gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd, act), Y)
+    assert all(torch.equal(p, q) for p, q in zip(gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, act), grads))
+
+
 @BOTH
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("n", [2, 200])
