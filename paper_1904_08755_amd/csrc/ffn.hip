@@ -22,6 +22,7 @@
 #include "ffn_act.h"
 #include "ffn_bf16.h"
 #include "ffn_f32.h"
+#include "ffn_mma.h"
 #include "ffn_res.h"
 
 namespace gsc {
@@ -313,6 +314,99 @@ k_ffn_gemm_bf16(const uint16_t* __restrict__ A1, const uint16_t* __restrict__ A2
     }
     store_tile(acc, r0 + 16 * MT * (wave / WN), c0 + 64 * (wave % WN), n, co, Out, co);
 }
+
+// The same for KC operands in tiles of 256 rows by 64 TN columns: eight waves of 64 x 32 TN (v_mfma_f32_32x32x16_bf16), a ring
+// of four stages of 32 reduction elements, each an array of its own: the operands are plain reads, which the compiler
+// starts ahead of the products without waiting for copies into other stages.
+template <int TN>
+__global__ void __launch_bounds__(512, 1)
+k_ffn_gemm_kc(const uint16_t* __restrict__ A1, const uint16_t* __restrict__ A2, int64_t lda, int64_t n, int64_t k,
+              const uint16_t* __restrict__ B1, const uint16_t* __restrict__ B2, int64_t ldb, int co,
+              uint16_t* __restrict__ Out, int nc) {
+    constexpr int BN = 64 * TN, STAGE = (256 + BN) * 64;
+    typedef FbCopy<false, 256, 8> CA;
+    typedef FbCopy<false, BN, 8> CB;
+    constexpr int LD = CA::N + CB::N;
+    __shared__ __attribute__((aligned(1024))) uint8_t slot0[STAGE];
+    __shared__ __attribute__((aligned(1024))) uint8_t slot1[STAGE];
+    __shared__ __attribute__((aligned(1024))) uint8_t slot2[STAGE];
+    __shared__ __attribute__((aligned(1024))) uint8_t slot3[STAGE];
+    auto slot = [&](auto N) -> uint8_t* {
+        constexpr int s = decltype(N)::value % 4;
+        return s == 0 ? slot0 : (s == 1 ? slot1 : (s == 2 ? slot2 : slot3));
+    };
+    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
+    const int64_t r0 = u / nc * 256;
+    const int c0 = (int)(u % nc) * BN;
+    const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
+    const FbSide a1{A1 + r0 * lda, lda, n - r0}, a2{A2 ? A2 + r0 * lda : nullptr, lda, n - r0};
+    const FbSide b1{B1 + (int64_t)c0 * ldb, ldb, co - c0}, b2{B2 ? B2 + (int64_t)c0 * ldb : nullptr, ldb, co - c0};
+    CA ca;
+    CB cb;
+    ca.start(a1, wave);
+    cb.start(b1, wave);
+    const int half = (int)((k + 31) / 32), steps = A2 ? 2 * half : half;
+    auto issue = [&](int s, uint8_t* dst) {
+        const bool second = s >= half;
+        const int64_t k0 = (int64_t)(second ? s - half : s) * 32;
+        ca.issue(second ? a2 : a1, k0, k, dst, wave);
+        cb.issue(second ? b2 : b1, k0, k, dst + CA::BYTES, wave);
+    };
+    const int i = threadIdx.x & 31, h = (threadIdx.x & 63) >> 5;
+    const int at = i * 64 + ((h ^ ((i >> 1) & 3)) * 16);   // elements 8 h .. of row i; 16 + 8 h .. at ^ 32
+    floatx16 acc[2][TN];
+#pragma unroll
+    for (int a = 0; a < 2; ++a)
+#pragma unroll
+        for (int b = 0; b < TN; ++b) acc[a][b] = floatx16{};
+    res_each<3>([&](auto N) {
+        if (decltype(N)::value < steps) issue(decltype(N)::value, slot(N));
+    });
+    for (int s4 = 0; s4 < steps; s4 += 4)
+        res_each<4>([&](auto N) {
+            const int s = s4 + decltype(N)::value;
+            if (s >= steps) return;
+            if (s + 2 < steps) fb_wait<2 * LD>();
+            else fb_wait<0>();
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the reads of the stage that is filled next are done
+            fb_barrier();
+            if (s + 3 < steps) issue(s + 3, slot(std::integral_constant<int, decltype(N)::value + 3>{}));
+            const uint8_t* la = slot(N) + wm * 4096;
+            const uint8_t* lb = slot(N) + CA::BYTES + wn * TN * 2048;
+            fbf16x8 a[2][2], b[2][TN];
+            auto read = [&](int kk) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m) a[kk][m] = *reinterpret_cast<const fbf16x8*>(la + m * 2048 + (at ^ (32 * kk)));
+#pragma unroll
+                for (int t = 0; t < TN; ++t) b[kk][t] = *reinterpret_cast<const fbf16x8*>(lb + t * 2048 + (at ^ (32 * kk)));
+            };
+            auto mul = [&](int kk) {
+#pragma unroll
+                for (int m = 0; m < 2; ++m)
+#pragma unroll
+                    for (int t = 0; t < TN; ++t) acc[m][t] = res_mma(b[kk][t], a[kk][m], acc[m][t]);
+            };
+            read(0);
+            read(1);
+            __builtin_amdgcn_sched_barrier(0);
+            mul(0);
+            mul(1);
+        });
+#pragma unroll
+    for (int m = 0; m < 2; ++m)
+#pragma unroll
+        for (int t = 0; t < TN; ++t) {
+            uint32_t o[8];
+#pragma unroll
+            for (int e = 0; e < 8; ++e) o[e] = pack_bf16(acc[m][t][2 * e], acc[m][t][2 * e + 1]);
+            res_store<false>(Out, co, r0 + 64 * wm + 32 * m, n, c0 + 32 * (TN * wn + t), co, o);
+        }
+}
+// (named: the host compilation leaves the second of two implicit instances out)
+template __global__ void k_ffn_gemm_kc<2>(const uint16_t*, const uint16_t*, int64_t, int64_t, int64_t, const uint16_t*,
+                                          const uint16_t*, int64_t, int, uint16_t*, int);
+template __global__ void k_ffn_gemm_kc<4>(const uint16_t*, const uint16_t*, int64_t, int64_t, int64_t, const uint16_t*,
+                                          const uint16_t*, int64_t, int, uint16_t*, int);
 
 // H (n x f8) and dG, dU (n x 2 f8, side by side) of a tile of 128 rows by 64 hidden columns.
 template <int MT>
@@ -665,6 +759,20 @@ static void ffn_dw(const FfnLayout& L, const DwSide<uint16_t>& p0, const DwSide<
                        L.per_chunk, part);
 }
 
+constexpr int64_t kGemmKcRows = 128 * 256;
+static void ffn_gemm_kc(const uint16_t* A1, const uint16_t* A2, int64_t lda, int64_t n, int64_t k, const uint16_t* B1,
+                        const uint16_t* B2, int64_t ldb, int co, uint16_t* Out, hipStream_t s) {
+    if (co <= 64 || n < kGemmKcRows) return ffn_gemm_bf16<FB_KC>(A1, A2, lda, n, k, B1, B2, ldb, co, Out, s);
+    auto launch = [&](auto TN) {
+        constexpr int tn = decltype(TN)::value;
+        const int nc = (int)ceil_div(co, 64 * tn);
+        hipLaunchKernelGGL(k_ffn_gemm_kc<tn>, dim3((unsigned)(ceil_div(n, 256) * nc)), dim3(512), 0, s, A1, A2, lda, n, k, B1,
+                           B2, ldb, co, Out, nc);
+    };
+    if (co > 128) launch(std::integral_constant<int, 4>{});
+    else launch(std::integral_constant<int, 2>{});
+}
+
 // --- either type
 // A few rows: H in float32.
 template <typename T>
@@ -709,7 +817,7 @@ static void ffn_bwd(const FfnShape& d, const FfnLayout& L, const T* X, const T* 
                 hipLaunchKernelGGL(k_ffn_mid_bf16<4>, dim3((unsigned)(ceil_div(n, 128) * nf)), dim3(256), 0, s, x.p, x.ld,
                                    y.p, y.ld, n, d.ci, d.co, g.p, u.p, g.ld, w.p, w.ld, d.f, act, H, dGU, (int)d.f8, nf);
             }
-            if (dX) ffn_gemm_bf16<FB_KC>(dGU, dGU + d.f8, 2 * d.f8, n, d.f, g.p, u.p, g.ld, d.ci, dX, s);
+            if (dX) ffn_gemm_kc(dGU, dGU + d.f8, 2 * d.f8, n, d.f, g.p, u.p, g.ld, d.ci, dX, s);
         } else {
             ffn_bwd_rows(d, L, X, Wg, Wu, Wd, dY, act, dX, ws, s);
         }
