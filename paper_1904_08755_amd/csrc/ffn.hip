@@ -96,10 +96,11 @@ __device__ __forceinline__ void store_tile(const floatx4 (&acc)[MT][NT], int64_t
     }
 }
 
+// H, dG and dU lie in blocks of 128 rows by 32 columns (row_blocks): a wave's 32 hidden columns are one block's.
 // H from gates (blocks 0, 1) and their partners (blocks 2, 3)
 template <typename T, int MT>
 __device__ __forceinline__ void store_hidden(const floatx4 (&acc)[MT][4], int64_t row0, int64_t col0, int64_t n, int act,
-                                             T* __restrict__ H, int64_t ldh) {
+                                             const RowMat<T>& H) {
     with_act(act, [&](auto ACT) {
 #pragma unroll
         for (int mi = 0; mi < MT; ++mi) {
@@ -113,16 +114,16 @@ __device__ __forceinline__ void store_hidden(const floatx4 (&acc)[MT][4], int64_
                     ffn_act<decltype(ACT)::value, false>(acc[mi][ni][e], a, d);
                     h[ni][e] = a * acc[mi][ni + 2][e];
                 }
-            store_pair(H + row * ldh, col0 + 4 * ffn_q(), ldh, row < n, h[0], h[1]);
+            store_pair(H.at(row, col0).p, 4 * ffn_q(), 32, row < n, h[0], h[1]);
         }
     });
 }
 
-// H, and dG and dU side by side, from gates, partners and dH
+// H, dG and dU from gates, partners and dH
 template <typename T, int MT>
 __device__ __forceinline__ void store_mid(const floatx4 (&acc)[MT][4], const floatx4 (&dh)[MT][2], int64_t row0,
-                                          int64_t col0, int64_t n, int act, T* __restrict__ H, T* __restrict__ dGU,
-                                          int64_t f8) {
+                                          int64_t col0, int64_t n, int act, const RowMat<T>& H, const RowMat<T>& dG,
+                                          const RowMat<T>& dU) {
     with_act(act, [&](auto ACT) {
 #pragma unroll
         for (int mi = 0; mi < MT; ++mi) {
@@ -139,10 +140,9 @@ __device__ __forceinline__ void store_mid(const floatx4 (&acc)[MT][4], const flo
                     dg[ni][e] = g * up * d;
                     du[ni][e] = g * a;
                 }
-            const int64_t col = col0 + 4 * ffn_q();
-            store_pair(H + row * f8, col, f8, row < n, h[0], h[1]);
-            store_pair(dGU + row * 2 * f8, col, f8, row < n, dg[0], dg[1]);
-            store_pair(dGU + row * 2 * f8 + f8, col, f8, row < n, du[0], du[1]);
+            store_pair(H.at(row, col0).p, 4 * ffn_q(), 32, row < n, h[0], h[1]);
+            store_pair(dG.at(row, col0).p, 4 * ffn_q(), 32, row < n, dg[0], dg[1]);
+            store_pair(dU.at(row, col0).p, 4 * ffn_q(), 32, row < n, du[0], du[1]);
         }
     });
 }
@@ -150,28 +150,27 @@ __device__ __forceinline__ void store_mid(const floatx4 (&acc)[MT][4], const flo
 // ---------------------------------------------------------------------------
 // float32 kernels: tiles of 32 MT rows
 // ---------------------------------------------------------------------------
-// H (n x ldh, columns behind f zero) of a tile by 64 hidden columns.
+// H (columns behind f zero) of a tile by 64 hidden columns.
 template <int MT>
 __global__ void __launch_bounds__(kFfnThreads, 2)
 k_ffn_up_f32(const float* __restrict__ X, int64_t n, int ci, const float* __restrict__ Wg, const float* __restrict__ Wu,
-             int f, int act, float* __restrict__ H, int64_t ldh, int nf) {
+             int f, int act, RowMat<float> H, int nf) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<MT, 4>()];
     const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
     const int64_t r0 = u / nf * (32 * MT);
     const int c0 = (int)(u % nf) * 64, wave = threadIdx.x >> 6;
     floatx4 acc[MT][4];
     zero_acc(acc);
-    tile_product<true, false, MT, 4, true>({X + r0 * ci, nullptr, ci, n - r0, ci}, {Wg + c0, Wu + c0, f, f - c0, ci},
-                                           lds, acc);
-    store_hidden(acc, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H, ldh);
+    tile_product<true, false, MT, 4, true>({row_major(X + r0 * ci, ci), nullptr, n - r0, ci},
+                                           {row_major(Wg + c0, f), Wu + c0, f - c0, ci}, lds, acc);
+    store_hidden(acc, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H);
 }
 
-// Out (n x co) = A1 B1 (+ A2 B2 where A2 is given): A rows of the reduction (KC), B either way.
+// Out (n x co) = A1 B1 (+ A2 B2 where A2 is given) over k: A rows of the reduction (KC), B (row-major) either way.
 template <bool BKC, int MT, int NT>
 __global__ void __launch_bounds__(kFfnThreads, 2)
-k_ffn_gemm_f32(const float* __restrict__ A1, const float* __restrict__ A2, int64_t lda, int64_t n, int64_t ka,
-               const float* __restrict__ B1, const float* __restrict__ B2, int64_t ldb, int64_t kb, int co,
-               float* __restrict__ Out, int nc) {
+k_ffn_gemm_f32(RowMat<const float> A1, RowMat<const float> A2, int64_t n, int64_t k, const float* __restrict__ B1,
+               const float* __restrict__ B2, int64_t ldb, int co, float* __restrict__ Out, int nc) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<MT, NT>()];
     const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
     const int64_t r0 = u / nc * (32 * MT);
@@ -179,21 +178,22 @@ k_ffn_gemm_f32(const float* __restrict__ A1, const float* __restrict__ A2, int64
     floatx4 acc[MT][NT];
     zero_acc(acc);
     for (int s = 0; s < 2; ++s) {
-        const float* A = s ? A2 : A1;
+        const RowMat<const float> A = s ? A2 : A1;
         const float* B = s ? B2 : B1;
-        if (!A) break;
-        tile_product<true, BKC, MT, NT, false>({A + r0 * lda, nullptr, lda, n - r0, ka},
-                                               {BKC ? B + (int64_t)c0 * ldb : B + c0, nullptr, ldb, co - c0, kb}, lds, acc);
+        if (!A.p) break;
+        tile_product<true, BKC, MT, NT, false>({A.at(r0, 0), nullptr, n - r0, k},
+                                               {row_major(BKC ? B + (int64_t)c0 * ldb : B + c0, ldb), nullptr, co - c0, k},
+                                               lds, acc);
     }
     store_tile(acc, r0 + 16 * MT * (wave >> 1), c0 + 16 * NT * (wave & 1), n, co, Out, co);
 }
 
-// H (n x f8) and dG, dU (n x 2 f8, side by side) of a tile by 64 hidden columns.
+// H, dG and dU of a tile by 64 hidden columns.
 template <int MT>
 __global__ void __launch_bounds__(kFfnThreads, 2)
 k_ffn_mid_f32(const float* __restrict__ X, const float* __restrict__ dY, int64_t n, int ci, int co,
               const float* __restrict__ Wg, const float* __restrict__ Wu, const float* __restrict__ Wd, int f, int act,
-              float* __restrict__ H, float* __restrict__ dGU, int f8, int nf) {
+              RowMat<float> H, RowMat<float> dG, RowMat<float> dU, int nf) {
     __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<MT, 4>()];
     const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
     const int64_t r0 = u / nf * (32 * MT);
@@ -201,19 +201,17 @@ k_ffn_mid_f32(const float* __restrict__ X, const float* __restrict__ dY, int64_t
     floatx4 acc[MT][4], dh[MT][2];
     zero_acc(acc);
     zero_acc(dh);
-    tile_product<true, false, MT, 4, true>({X + r0 * ci, nullptr, ci, n - r0, ci}, {Wg + c0, Wu + c0, f, f - c0, ci},
-                                           lds, acc);
-    tile_product<true, true, MT, 2, false>({dY + r0 * co, nullptr, co, n - r0, co},
-                                           {Wd + (int64_t)c0 * co, nullptr, co, f - c0, co}, lds, dh);
-    store_mid(acc, dh, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H, dGU, f8);
+    tile_product<true, false, MT, 4, true>({row_major(X + r0 * ci, ci), nullptr, n - r0, ci},
+                                           {row_major(Wg + c0, f), Wu + c0, f - c0, ci}, lds, acc);
+    tile_product<true, true, MT, 2, false>({row_major(dY + r0 * co, co), nullptr, n - r0, co},
+                                           {row_major(Wd + (int64_t)c0 * co, co), nullptr, f - c0, co}, lds, dh);
+    store_mid(acc, dh, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H, dG, dU);
 }
 
-// One product of k_ffn_dw: out (m x nn) = A^T B over the rows, A n x lda, B n x ldb.
+// One product of k_ffn_dw: out (m x nn) = A^T B over the rows.
 template <typename T>
 struct DwSide {
-    const T* A;
-    const T* B;
-    int64_t lda, ldb;
+    RowMat<const T> A, B;
     int m, nn;
     int tn, tiles;     // column tiles, all tiles (0: the product is not wanted)
     int64_t part;      // where its sums start in a chunk's partial sums
@@ -235,8 +233,8 @@ k_ffn_dw_f32(DwSide<float> p0, DwSide<float> p1, int64_t n, int64_t chunk, int64
     const int64_t r0 = s * chunk, rows = n - r0 < chunk ? n - r0 : chunk;
     floatx4 acc[MT][NT];
     zero_acc(acc);
-    tile_product<false, false, MT, NT, false>({p.A + r0 * p.lda + m0, nullptr, p.lda, p.m - m0, rows},
-                                              {p.B + r0 * p.ldb + c0, nullptr, p.ldb, p.nn - c0, rows}, lds, acc);
+    tile_product<false, false, MT, NT, false>({p.A.at(r0, m0), nullptr, p.m - m0, rows},
+                                              {p.B.at(r0, c0), nullptr, p.nn - c0, rows}, lds, acc);
     store_tile(acc, m0 + 16 * MT * (wave >> 1), c0 + 16 * NT * (wave & 1), p.m, p.nn, part + s * per_chunk + p.part, p.nn);
 }
 
@@ -274,11 +272,11 @@ __global__ void __launch_bounds__(kFfnThreads) k_ffn_pad(FfnPad p) {
     }
 }
 
-// H (n x ldh) of a tile of 32 MT rows by 64 hidden columns.
+// H of a tile of 32 MT rows by 64 hidden columns.
 template <int MT>
 __global__ void __launch_bounds__(256, 2)
 k_ffn_up_bf16(const uint16_t* __restrict__ X, int64_t ldx, int64_t n, int ci, const uint16_t* __restrict__ Wg,
-              const uint16_t* __restrict__ Wu, int64_t ldw, int f, int act, uint16_t* __restrict__ H, int64_t ldh, int nf) {
+              const uint16_t* __restrict__ Wu, int64_t ldw, int f, int act, RowMat<uint16_t> H, int nf) {
     typedef FbShape<2, 2, MT, 4> S;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
     const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
@@ -286,16 +284,16 @@ k_ffn_up_bf16(const uint16_t* __restrict__ X, int64_t ldx, int64_t n, int ci, co
     const int c0 = (int)(u % nf) * 64, wave = threadIdx.x >> 6;
     floatx4 acc[MT][4];
     zero_acc(acc);
-    fb_product<2, 2, MT, 4, false, FB_PAIR>({X + r0 * ldx, ldx, n - r0}, {Wg + c0, ldw, f - c0}, Wu + c0, ci, lds, acc);
-    store_hidden(acc, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H, ldh);
+    fb_product<2, 2, MT, 4, FB_KC, FB_MC, true>({row_major(X + r0 * ldx, ldx), n - r0}, {row_major(Wg + c0, ldw), f - c0},
+                                                Wu + c0, ci, lds, acc);
+    store_hidden(acc, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H);
 }
 
 // Out (n x co, rows as they are) = A1 B1 (+ A2 B2 where A2 is given) over k.
-template <int WM, int WN, int MT, FbB BK>
+template <int WM, int WN, int MT, FbLay BL>
 __global__ void __launch_bounds__(256, 2)
-k_ffn_gemm_bf16(const uint16_t* __restrict__ A1, const uint16_t* __restrict__ A2, int64_t lda, int64_t n, int64_t k,
-                const uint16_t* __restrict__ B1, const uint16_t* __restrict__ B2, int64_t ldb, int co,
-                uint16_t* __restrict__ Out, int nc) {
+k_ffn_gemm_bf16(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, int64_t k, const uint16_t* __restrict__ B1,
+                const uint16_t* __restrict__ B2, int64_t ldb, int co, uint16_t* __restrict__ Out, int nc) {
     typedef FbShape<WM, WN, MT, 4> S;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
     const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
@@ -304,28 +302,27 @@ k_ffn_gemm_bf16(const uint16_t* __restrict__ A1, const uint16_t* __restrict__ A2
     floatx4 acc[MT][4];
     zero_acc(acc);
     for (int s = 0; s < 2; ++s) {
-        const uint16_t* A = s ? A2 : A1;
+        const RowMat<const uint16_t> A = s ? A2 : A1;
         const uint16_t* B = s ? B2 : B1;
-        if (!A) break;
+        if (!A.p) break;
         if (s) fb_barrier();   // the first product's last reads
-        fb_product<WM, WN, MT, 4, false, BK>({A + r0 * lda, lda, n - r0},
-                                             {BK == FB_KC ? B + (int64_t)c0 * ldb : B + c0, ldb, co - c0}, nullptr, k, lds,
-                                             acc);
+        fb_product<WM, WN, MT, 4, FB_KC, BL>({A.at(r0, 0), n - r0},
+                                             {row_major(BL == FB_KC ? B + (int64_t)c0 * ldb : B + c0, ldb), co - c0}, nullptr, k,
+                                             lds, acc);
     }
     store_tile(acc, r0 + 16 * MT * (wave / WN), c0 + 64 * (wave % WN), n, co, Out, co);
 }
 
-// The same for KC operands in tiles of 256 rows by 64 TN columns: eight waves of 64 x 32 TN (v_mfma_f32_32x32x16_bf16), a ring
+// Out (n x co) = A1 B1 + A2 B2 for KC operands in tiles of 256 rows by 64 TN columns: eight waves of 64 x 32 TN (v_mfma_f32_32x32x16_bf16), a ring
 // of four stages of 32 reduction elements, each an array of its own: the operands are plain reads, which the compiler
 // starts ahead of the products without waiting for copies into other stages.
 template <int TN>
 __global__ void __launch_bounds__(512, 1)
-k_ffn_gemm_kc(const uint16_t* __restrict__ A1, const uint16_t* __restrict__ A2, int64_t lda, int64_t n, int64_t k,
-              const uint16_t* __restrict__ B1, const uint16_t* __restrict__ B2, int64_t ldb, int co,
-              uint16_t* __restrict__ Out, int nc) {
+k_ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, int64_t k, const uint16_t* __restrict__ B1,
+              const uint16_t* __restrict__ B2, int64_t ldb, int co, uint16_t* __restrict__ Out, int nc) {
     constexpr int BN = 64 * TN, STAGE = (256 + BN) * 64;
-    typedef FbCopy<false, 256, 8> CA;
-    typedef FbCopy<false, BN, 8> CB;
+    typedef FbCopy<FB_KC, 256, 8> CA;
+    typedef FbCopy<FB_KC, BN, 8> CB;
     constexpr int LD = CA::N + CB::N;
     __shared__ __attribute__((aligned(1024))) uint8_t slot0[STAGE];
     __shared__ __attribute__((aligned(1024))) uint8_t slot1[STAGE];
@@ -339,13 +336,13 @@ k_ffn_gemm_kc(const uint16_t* __restrict__ A1, const uint16_t* __restrict__ A2, 
     const int64_t r0 = u / nc * 256;
     const int c0 = (int)(u % nc) * BN;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
-    const FbSide a1{A1 + r0 * lda, lda, n - r0}, a2{A2 ? A2 + r0 * lda : nullptr, lda, n - r0};
-    const FbSide b1{B1 + (int64_t)c0 * ldb, ldb, co - c0}, b2{B2 ? B2 + (int64_t)c0 * ldb : nullptr, ldb, co - c0};
+    const FbSide a1{A1.at(r0, 0), n - r0}, a2{A2.at(r0, 0), n - r0};
+    const FbSide b1{row_major(B1 + (int64_t)c0 * ldb, ldb), co - c0}, b2{row_major(B2 + (int64_t)c0 * ldb, ldb), co - c0};
     CA ca;
     CB cb;
     ca.start(a1, wave);
     cb.start(b1, wave);
-    const int half = (int)((k + 31) / 32), steps = A2 ? 2 * half : half;
+    const int half = (int)((k + 31) / 32), steps = 2 * half;
     auto issue = [&](int s, uint8_t* dst) {
         const bool second = s >= half;
         const int64_t k0 = (int64_t)(second ? s - half : s) * 32;
@@ -359,39 +356,49 @@ k_ffn_gemm_kc(const uint16_t* __restrict__ A1, const uint16_t* __restrict__ A2, 
     for (int a = 0; a < 2; ++a)
 #pragma unroll
         for (int b = 0; b < TN; ++b) acc[a][b] = floatx16{};
-    res_each<3>([&](auto N) {
-        if (decltype(N)::value < steps) issue(decltype(N)::value, slot(N));
-    });
+    // During step s the copies of step s + 4 are started into the stage that step s's operands came from, the operands of
+    // step s + 1 are read, and the products of step s run on those read during step s - 1.
+    fbf16x8 fa[2][2][2], fb[2][2][TN];   // of even and odd steps: 16 reduction elements twice
+    auto read = [&](auto N, fbf16x8 (&a)[2][2], fbf16x8 (&b)[2][TN]) {
+        const uint8_t* la = slot(N) + wm * 4096;
+        const uint8_t* lb = slot(N) + CA::BYTES + wn * TN * 2048;
+#pragma unroll
+        for (int kk = 0; kk < 2; ++kk) {
+#pragma unroll
+            for (int m = 0; m < 2; ++m) a[kk][m] = *reinterpret_cast<const fbf16x8*>(la + m * 2048 + (at ^ (32 * kk)));
+#pragma unroll
+            for (int t = 0; t < TN; ++t) b[kk][t] = *reinterpret_cast<const fbf16x8*>(lb + t * 2048 + (at ^ (32 * kk)));
+        }
+    };
+    // The next stage has landed for all waves, two later ones are in flight; all LDS reads before are done.  (Beyond the end
+    // copies that carry nothing are started, so that their number is the same everywhere: with branches around them the
+    // compiler cannot tell which have landed and waits for all of them before it reads a stage.)
+    auto land = [&] {
+        fb_wait<2 * LD>();
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        fb_barrier();
+    };
+    res_each<3>([&](auto N) { issue(decltype(N)::value, slot(N)); });
+    land();
+    issue(3, slot(std::integral_constant<int, 3>{}));
+    read(std::integral_constant<int, 0>{}, fa[0], fb[0]);
     for (int s4 = 0; s4 < steps; s4 += 4)
         res_each<4>([&](auto N) {
-            const int s = s4 + decltype(N)::value;
-            if (s >= steps) return;
-            if (s + 2 < steps) fb_wait<2 * LD>();
-            else fb_wait<0>();
-            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // the reads of the stage that is filled next are done
-            fb_barrier();
-            if (s + 3 < steps) issue(s + 3, slot(std::integral_constant<int, decltype(N)::value + 3>{}));
-            const uint8_t* la = slot(N) + wm * 4096;
-            const uint8_t* lb = slot(N) + CA::BYTES + wn * TN * 2048;
-            fbf16x8 a[2][2], b[2][TN];
-            auto read = [&](int kk) {
+            constexpr int v = decltype(N)::value;
+            land();
+            issue(s4 + v + 4, slot(N));
+            __builtin_amdgcn_sched_barrier(0);
+            read(std::integral_constant<int, v + 1>{}, fa[(v + 1) & 1], fb[(v + 1) & 1]);
+            __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-                for (int m = 0; m < 2; ++m) a[kk][m] = *reinterpret_cast<const fbf16x8*>(la + m * 2048 + (at ^ (32 * kk)));
-#pragma unroll
-                for (int t = 0; t < TN; ++t) b[kk][t] = *reinterpret_cast<const fbf16x8*>(lb + t * 2048 + (at ^ (32 * kk)));
-            };
-            auto mul = [&](int kk) {
+            for (int kk = 0; kk < 2; ++kk)
 #pragma unroll
                 for (int m = 0; m < 2; ++m)
 #pragma unroll
-                    for (int t = 0; t < TN; ++t) acc[m][t] = res_mma(b[kk][t], a[kk][m], acc[m][t]);
-            };
-            read(0);
-            read(1);
+                    for (int t = 0; t < TN; ++t) acc[m][t] = res_mma(fb[v & 1][kk][t], fa[v & 1][kk][m], acc[m][t]);
             __builtin_amdgcn_sched_barrier(0);
-            mul(0);
-            mul(1);
         });
+    fb_wait<0>();   // no copy is in flight when the block ends
 #pragma unroll
     for (int m = 0; m < 2; ++m)
 #pragma unroll
@@ -403,18 +410,18 @@ k_ffn_gemm_kc(const uint16_t* __restrict__ A1, const uint16_t* __restrict__ A2, 
         }
 }
 // (named: the host compilation leaves the second of two implicit instances out)
-template __global__ void k_ffn_gemm_kc<2>(const uint16_t*, const uint16_t*, int64_t, int64_t, int64_t, const uint16_t*,
+template __global__ void k_ffn_gemm_kc<2>(RowMat<const uint16_t>, RowMat<const uint16_t>, int64_t, int64_t, const uint16_t*,
                                           const uint16_t*, int64_t, int, uint16_t*, int);
-template __global__ void k_ffn_gemm_kc<4>(const uint16_t*, const uint16_t*, int64_t, int64_t, int64_t, const uint16_t*,
+template __global__ void k_ffn_gemm_kc<4>(RowMat<const uint16_t>, RowMat<const uint16_t>, int64_t, int64_t, const uint16_t*,
                                           const uint16_t*, int64_t, int, uint16_t*, int);
 
-// H (n x f8) and dG, dU (n x 2 f8, side by side) of a tile of 128 rows by 64 hidden columns.
+// H, dG and dU of a tile of 128 rows by 64 hidden columns.
 template <int MT>
 __global__ void __launch_bounds__(256, 2)
 k_ffn_mid_bf16(const uint16_t* __restrict__ X, int64_t ldx, const uint16_t* __restrict__ dY, int64_t ldy, int64_t n, int ci,
                int co, const uint16_t* __restrict__ Wg, const uint16_t* __restrict__ Wu, int64_t ldw,
-               const uint16_t* __restrict__ Wd, int64_t ldd, int f, int act, uint16_t* __restrict__ H,
-               uint16_t* __restrict__ dGU, int f8, int nf) {
+               const uint16_t* __restrict__ Wd, int64_t ldd, int f, int act, RowMat<uint16_t> H, RowMat<uint16_t> dG,
+               RowMat<uint16_t> dU, int nf) {
     typedef FbShape<2, 2, MT, 4> S;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
     const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
@@ -423,22 +430,22 @@ k_ffn_mid_bf16(const uint16_t* __restrict__ X, int64_t ldx, const uint16_t* __re
     floatx4 acc[MT][4], dh[MT][2];
     zero_acc(acc);
     zero_acc(dh);
-    fb_product<2, 2, MT, 4, false, FB_PAIR>({X + r0 * ldx, ldx, n - r0}, {Wg + c0, ldw, f - c0}, Wu + c0, ci, lds, acc);
+    fb_product<2, 2, MT, 4, FB_KC, FB_MC, true>({row_major(X + r0 * ldx, ldx), n - r0}, {row_major(Wg + c0, ldw), f - c0},
+                                                Wu + c0, ci, lds, acc);
     fb_barrier();
-    fb_product<2, 2, MT, 2, false, FB_KC>({dY + r0 * ldy, ldy, n - r0}, {Wd + (int64_t)c0 * ldd, ldd, f - c0}, nullptr, co,
-                                          lds, dh);
-    store_mid(acc, dh, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H, dGU, f8);
+    fb_product<2, 2, MT, 2, FB_KC, FB_KC>({row_major(dY + r0 * ldy, ldy), n - r0},
+                                          {row_major(Wd + (int64_t)c0 * ldd, ldd), f - c0}, nullptr, co, lds, dh);
+    store_mid(acc, dh, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H, dG, dU);
 }
 
-template <int WM, int WN, int MT>
+template <int WM, int WN, int MT, FbLay AL, FbLay BL>
 __device__ __forceinline__ void dw_tile(const DwSide<uint16_t>& p, int t, int64_t r0, int64_t rows, uint8_t* lds,
                                         float* __restrict__ part) {
     typedef FbShape<WM, WN, MT, 4> S;
     const int m0 = t / p.tn * S::BM, c0 = t % p.tn * S::BN, wave = threadIdx.x >> 6;
     floatx4 acc[MT][4];
     zero_acc(acc);
-    fb_product<WM, WN, MT, 4, true, FB_MC>({p.A + r0 * p.lda + m0, p.lda, p.m - m0},
-                                           {p.B + r0 * p.ldb + c0, p.ldb, p.nn - c0}, nullptr, rows, lds, acc);
+    fb_product<WM, WN, MT, 4, AL, BL>({p.A.at(r0, m0), p.m - m0}, {p.B.at(r0, c0), p.nn - c0}, nullptr, rows, lds, acc);
     store_tile(acc, m0 + 16 * MT * (wave / WN), c0 + 64 * (wave % WN), p.m, p.nn, part + p.part, p.nn);
 }
 
@@ -458,24 +465,24 @@ k_ffn_dw_bf16(DwSide<uint16_t> p0, DwSide<uint16_t> p1, int64_t n, int64_t chunk
     const int t = (int)(u - s * tiles);
     const int64_t r0 = s * chunk, rows = n - r0 < chunk ? n - r0 : chunk;
     float* out = part + s * per_chunk;
-    if (t < p0.tiles) dw_tile<1, 4, MT0>(p0, t, r0, rows, lds, out);
-    else dw_tile<WM1, WN1, MT1>(p1, t - p0.tiles, r0, rows, lds, out);
+    if (t < p0.tiles) dw_tile<1, 4, MT0, FB_MC, FB_MB>(p0, t, r0, rows, lds, out);
+    else dw_tile<WM1, WN1, MT1, FB_MB, FB_MC>(p1, t - p0.tiles, r0, rows, lds, out);
 }
 
-// The weights' gradients from the chunks' sums, added in chunk order: per chunk dWg | dWu as ci x 2 f8, then dWd.
+// The weights' gradients from the chunks' sums, added in chunk order: per chunk dWg | dWu as ci x 2 fp, then dWd.
 template <typename T>
 __global__ void __launch_bounds__(kFfnThreads)
-k_ffn_dw_sum(const float* __restrict__ part, int64_t chunks, int64_t per_chunk, int ci, int f, int f8, int co,
+k_ffn_dw_sum(const float* __restrict__ part, int64_t chunks, int64_t per_chunk, int ci, int f, int fp, int co,
              T* __restrict__ dWg, T* __restrict__ dWu, T* __restrict__ dWd, int64_t up, int64_t total) {
     for (int64_t i = (int64_t)blockIdx.x * kFfnThreads + threadIdx.x; i < total; i += (int64_t)gridDim.x * kFfnThreads) {
         T* out;
         if (i < up) {
-            const int64_t row = i / (2 * f8);
-            int col = (int)(i - row * 2 * f8);
+            const int64_t row = i / (2 * fp);
+            int col = (int)(i - row * 2 * fp);
             out = dWg;
-            if (col >= f8) {
+            if (col >= fp) {
                 out = dWu;
-                col -= f8;
+                col -= fp;
             }
             if (!out || col >= f) continue;
             out += row * f + col;
@@ -572,8 +579,8 @@ static bool ffn_sizes_ok(int32_t dtype, int64_t n, int32_t ci, int32_t f, int32_
 struct FfnShape {
     int64_t n;
     int ci, f, co;
-    int64_t f8;
-    FfnShape(int64_t n, int ci, int f, int co) : n(n), ci(ci), f(f), co(co), f8(pad8(f)) {}
+    int64_t fp;   // hidden columns in whole tiles
+    FfnShape(int64_t n, int ci, int f, int co) : n(n), ci(ci), f(f), co(co), fp(ceil_div(f, 64) * 64) {}
 };
 
 // Workspace, in order: what the padded copies of X, dY (backward), Wg, Wu and Wd and the packed weights take
@@ -617,14 +624,15 @@ static FfnLayout ffn_layout(int dtype, const FfnShape& d, bool bwd) {
     if (dtype == GSC_BF16) {
         L.x = take((size_t)d.n * pad8(d.ci) * 2);
         if (bwd) L.dy = take((size_t)d.n * pad8(d.co) * 2);
-        L.wg = take((size_t)d.ci * d.f8 * 2);
-        L.wu = take((size_t)d.ci * d.f8 * 2);
+        L.wg = take((size_t)d.ci * pad8(d.f) * 2);
+        L.wu = take((size_t)d.ci * pad8(d.f) * 2);
         L.wd = take((size_t)d.f * pad8(d.co) * 2);
         if (ffn_resident(d, bwd)) L.pack = take(res_pack_bytes(d.ci, d.f, d.co, bwd));
     }
-    L.h = take((size_t)d.n * d.f8 * (d.n <= kFfnFewRows ? 4 : size));
+    const int64_t tiles = ceil_div(d.n, 128);
+    L.h = take((size_t)(!bwd && d.n <= kFfnFewRows ? d.n * 4 : tiles * 128 * size) * d.fp);
     if (bwd) {
-        L.dgu = take((size_t)d.n * 2 * d.f8 * size);
+        L.dgu = take((size_t)tiles * 128 * 2 * d.fp * size);
         int bm0, bn0, bm1, bn1;
         if (dtype == GSC_BF16) {
             L.m_nar = d.ci <= 64;
@@ -638,13 +646,13 @@ static FfnLayout ffn_layout(int dtype, const FfnShape& d, bool bwd) {
             bm0 = bm1 = L.m_nar ? 64 : 128;
             bn0 = bn1 = L.n_nar ? 64 : 128;
         }
-        L.tn0 = (int)ceil_div(2 * d.f8, bn0);
+        L.tn0 = (int)ceil_div(2 * d.fp, bn0);
         L.t0 = (int)ceil_div(d.ci, bm0) * L.tn0;
         L.tn1 = (int)ceil_div(d.co, bn1);
         L.t1 = (int)ceil_div(d.f, bm1) * L.tn1;
-        L.chunk = ceil_div(ceil_div(rows, ffn_chunks(d.n, (int64_t)L.t0 + L.t1)), 64) * 64;
+        L.chunk = ceil_div(ceil_div(rows, ffn_chunks(d.n, (int64_t)L.t0 + L.t1)), 128) * 128;
         L.chunks = ceil_div(rows, L.chunk);
-        L.up = (int64_t)d.ci * 2 * d.f8;
+        L.up = (int64_t)d.ci * 2 * d.fp;
         L.per_chunk = L.up + (int64_t)d.f * d.co;
         L.part = take((size_t)L.chunks * L.per_chunk * sizeof(float));
     }
@@ -655,40 +663,42 @@ static FfnLayout ffn_layout(int dtype, const FfnShape& d, bool bwd) {
 // Row tiles of 64 (float32) or 128 (bfloat16) instead of twice as many where those would leave compute units idle.
 static bool ffn_short(int64_t n, int rows, int64_t col_tiles) { return ceil_div(n, rows) * col_tiles < 2 * device_cus(); }
 
+template <typename T>
+static RowMat<const T> ffn_const(const RowMat<T>& m) { return {m.p, m.ld, m.gs, m.ts}; }
+
 // --- float32
 template <bool BKC>
-static void ffn_gemm_f32(const float* A1, const float* A2, int64_t lda, int64_t n, int64_t ka, const float* B1,
-                         const float* B2, int64_t ldb, int64_t kb, int co, float* Out, hipStream_t s) {
+static void ffn_gemm_f32(RowMat<const float> A1, RowMat<const float> A2, int64_t n, int64_t k, const float* B1,
+                         const float* B2, int64_t ldb, int co, float* Out, hipStream_t s) {
     const bool nar = ffn_narrow(co);
     const int nc = (int)ceil_div(co, nar ? 64 : 128);
     const bool sho = ffn_short(n, 128, nc);
     auto* kern = sho ? (nar ? k_ffn_gemm_f32<BKC, 2, 2> : k_ffn_gemm_f32<BKC, 2, 4>)
                      : (nar ? k_ffn_gemm_f32<BKC, 4, 2> : k_ffn_gemm_f32<BKC, 4, 4>);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(n, sho ? 64 : 128) * nc)), dim3(kFfnThreads), 0, s, A1, A2, lda,
-                       n, ka, B1, B2, ldb, kb, co, Out, nc);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(n, sho ? 64 : 128) * nc)), dim3(kFfnThreads), 0, s, A1, A2, n, k,
+                       B1, B2, ldb, co, Out, nc);
 }
 
 static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const float* X, const float* Wg, const float* Wu,
                     const float* Wd, int act, float* Y, char* ws, hipStream_t s) {
-    float* H = reinterpret_cast<float*>(ws + L.h);
+    const RowMat<float> H = row_blocks(reinterpret_cast<float*>(ws + L.h), d.fp);
     const int nf = (int)ceil_div(d.f, 64);
     const bool sho = ffn_short(d.n, 128, nf);
     auto* up = sho ? k_ffn_up_f32<2> : k_ffn_up_f32<4>;
     hipLaunchKernelGGL(up, dim3((unsigned)(ceil_div(d.n, sho ? 64 : 128) * nf)), dim3(kFfnThreads), 0, s, X, d.n, d.ci, Wg,
-                       Wu, d.f, act, H, d.f8, nf);
-    ffn_gemm_f32<false>(H, nullptr, d.f8, d.n, d.f8, Wd, nullptr, d.co, d.f, d.co, Y, s);
+                       Wu, d.f, act, H, nf);
+    ffn_gemm_f32<false>(ffn_const(H), {}, d.n, d.f, Wd, nullptr, d.co, d.co, Y, s);
 }
 
-static void ffn_bwd_rows(const FfnShape& d, const FfnLayout& L, const float* X, const float* Wg, const float* Wu,
-                         const float* Wd, const float* dY, int act, float* dX, char* ws, hipStream_t s) {
-    float* H = reinterpret_cast<float*>(ws + L.h);
-    float* dGU = reinterpret_cast<float*>(ws + L.dgu);
+static void ffn_bwd_rows(const FfnShape& d, const float* X, const float* Wg, const float* Wu, const float* Wd,
+                         const float* dY, int act, float* dX, RowMat<float> H, RowMat<float> dG, RowMat<float> dU,
+                         hipStream_t s) {
     const int nf = (int)ceil_div(d.f, 64);
     const bool sho = ffn_short(d.n, 128, nf);
     auto* mid = sho ? k_ffn_mid_f32<2> : k_ffn_mid_f32<4>;
     hipLaunchKernelGGL(mid, dim3((unsigned)(ceil_div(d.n, sho ? 64 : 128) * nf)), dim3(kFfnThreads), 0, s, X, dY, d.n,
-                       d.ci, d.co, Wg, Wu, Wd, d.f, act, H, dGU, (int)d.f8, nf);
-    if (dX) ffn_gemm_f32<true>(dGU, dGU + d.f8, 2 * d.f8, d.n, d.f8, Wg, Wu, d.f, d.f, d.ci, dX, s);
+                       d.ci, d.co, Wg, Wu, Wd, d.f, act, H, dG, dU, nf);
+    if (dX) ffn_gemm_f32<true>(ffn_const(dG), ffn_const(dU), d.n, d.f, Wg, Wu, d.f, d.ci, dX, s);
 }
 
 static void ffn_dw(const FfnLayout& L, const DwSide<float>& p0, const DwSide<float>& p1, int64_t n, float* part,
@@ -721,20 +731,20 @@ static void ffn_pad(const FfnPad& pad, hipStream_t s) {
     hipLaunchKernelGGL(k_ffn_pad, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kFfnThreads), 0, s, pad);
 }
 
-template <FbB BK>
-static void ffn_gemm_bf16(const uint16_t* A1, const uint16_t* A2, int64_t lda, int64_t n, int64_t k, const uint16_t* B1,
+template <FbLay BL>
+static void ffn_gemm_bf16(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, int64_t k, const uint16_t* B1,
                           const uint16_t* B2, int64_t ldb, int co, uint16_t* Out, hipStream_t s) {
     const bool nar = co <= 64;
     const int nc = (int)ceil_div(co, nar ? 64 : 128);
     const bool sho = !nar && ffn_short(n, 256, nc);
-    auto* kern = nar ? k_ffn_gemm_bf16<4, 1, 4, BK> : (sho ? k_ffn_gemm_bf16<2, 2, 4, BK> : k_ffn_gemm_bf16<2, 2, 8, BK>);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(n, sho ? 128 : 256) * nc)), dim3(256), 0, s, A1, A2, lda, n, k, B1,
-                       B2, ldb, co, Out, nc);
+    auto* kern = nar ? k_ffn_gemm_bf16<4, 1, 4, BL> : (sho ? k_ffn_gemm_bf16<2, 2, 4, BL> : k_ffn_gemm_bf16<2, 2, 8, BL>);
+    hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(n, sho ? 128 : 256) * nc)), dim3(256), 0, s, A1, A2, n, k, B1, B2, ldb,
+                       co, Out, nc);
 }
 
 static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const uint16_t* X, const uint16_t* Wg, const uint16_t* Wu,
                     const uint16_t* Wd, int act, uint16_t* Y, char* ws, hipStream_t s) {
-    uint16_t* H = reinterpret_cast<uint16_t*>(ws + L.h);
+    const RowMat<uint16_t> H = row_blocks(reinterpret_cast<uint16_t*>(ws + L.h), d.fp);
     if (ffn_resident(d, false)) {
         res_fwd(X, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, Y, ws + L.pack, s);
         return;
@@ -747,8 +757,8 @@ static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const uint16_t* X, co
     const bool sho = ffn_short(d.n, 256, nf);
     auto* up = sho ? k_ffn_up_bf16<4> : k_ffn_up_bf16<8>;
     hipLaunchKernelGGL(up, dim3((unsigned)(ceil_div(d.n, sho ? 128 : 256) * nf)), dim3(256), 0, s, x.p, x.ld, d.n, d.ci,
-                       g.p, u.p, g.ld, d.f, act, H, d.f8, nf);
-    ffn_gemm_bf16<FB_MC>(H, nullptr, d.f8, d.n, d.f, w.p, nullptr, w.ld, d.co, Y, s);
+                       g.p, u.p, g.ld, d.f, act, H, nf);
+    ffn_gemm_bf16<FB_MC>(ffn_const(H), {}, d.n, d.f, w.p, nullptr, w.ld, d.co, Y, s);
 }
 
 static void ffn_dw(const FfnLayout& L, const DwSide<uint16_t>& p0, const DwSide<uint16_t>& p1, int64_t n, float* part,
@@ -760,14 +770,14 @@ static void ffn_dw(const FfnLayout& L, const DwSide<uint16_t>& p0, const DwSide<
 }
 
 constexpr int64_t kGemmKcRows = 128 * 256;
-static void ffn_gemm_kc(const uint16_t* A1, const uint16_t* A2, int64_t lda, int64_t n, int64_t k, const uint16_t* B1,
+static void ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, int64_t k, const uint16_t* B1,
                         const uint16_t* B2, int64_t ldb, int co, uint16_t* Out, hipStream_t s) {
-    if (co <= 64 || n < kGemmKcRows) return ffn_gemm_bf16<FB_KC>(A1, A2, lda, n, k, B1, B2, ldb, co, Out, s);
+    if (co <= 64 || n < kGemmKcRows) return ffn_gemm_bf16<FB_KC>(A1, A2, n, k, B1, B2, ldb, co, Out, s);
     auto launch = [&](auto TN) {
         constexpr int tn = decltype(TN)::value;
         const int nc = (int)ceil_div(co, 64 * tn);
-        hipLaunchKernelGGL(k_ffn_gemm_kc<tn>, dim3((unsigned)(ceil_div(n, 256) * nc)), dim3(512), 0, s, A1, A2, lda, n, k, B1,
-                           B2, ldb, co, Out, nc);
+        hipLaunchKernelGGL(k_ffn_gemm_kc<tn>, dim3((unsigned)(ceil_div(n, 256) * nc)), dim3(512), 0, s, A1, A2, n, k, B1, B2, ldb, co,
+                           Out, nc);
     };
     if (co > 128) launch(std::integral_constant<int, 4>{});
     else launch(std::integral_constant<int, 2>{});
@@ -785,8 +795,8 @@ static void ffn_fwd_few(const FfnShape& d, const FfnLayout& L, const T* X, const
     auto* down = n == 1 ? k_ffn_few<float, T, T, 1, false>
                         : (n == 2 ? k_ffn_few<float, T, T, 2, false> : k_ffn_few<float, T, T, 4, false>);
     hipLaunchKernelGGL(up, dim3((unsigned)ceil_div(d.f, W)), dim3(kFfnThreads), 0, s, X, (int64_t)d.ci, n, d.ci, Wg, Wu,
-                       d.f, act, H, d.f8);
-    hipLaunchKernelGGL(down, dim3((unsigned)ceil_div(d.co, W)), dim3(kFfnThreads), 0, s, (const float*)H, d.f8, n, d.f, Wd,
+                       d.f, act, H, d.fp);
+    hipLaunchKernelGGL(down, dim3((unsigned)ceil_div(d.co, W)), dim3(kFfnThreads), 0, s, (const float*)H, d.fp, n, d.f, Wd,
                        (const T*)nullptr, d.co, act, Y, (int64_t)d.co);
 }
 
@@ -794,8 +804,9 @@ template <typename T>
 static void ffn_bwd(const FfnShape& d, const FfnLayout& L, const T* X, const T* Wg, const T* Wu, const T* Wd, const T* dY,
                     int act, T* dX, T* dWg, T* dWu, T* dWd, char* ws, hipStream_t s) {
     const int64_t n = d.n;
-    T* H = reinterpret_cast<T*>(ws + L.h);
-    T* dGU = reinterpret_cast<T*>(ws + L.dgu);
+    // dG and dU share their blocks of 128 rows: the gradients of both projections are one product with X
+    const RowMat<T> H = row_blocks(reinterpret_cast<T*>(ws + L.h), d.fp),
+                    dG = row_blocks(reinterpret_cast<T*>(ws + L.dgu), 2 * d.fp), dU = dG.at(0, d.fp);
     float* part = reinterpret_cast<float*>(ws + L.part);
     const T *xs = X, *ys = dY;
     int64_t ldx = d.ci, ldy = d.co;
@@ -812,25 +823,25 @@ static void ffn_bwd(const FfnShape& d, const FfnLayout& L, const T* X, const T* 
             ldy = y.ld;
             const int nf = (int)ceil_div(d.f, 64);
             if (ffn_resident(d, true)) {
-                res_mid(X, dY, n, d.ci, Wg, Wu, d.f, Wd, d.co, act, H, dGU, d.f8, ws + L.pack, s);
+                res_mid(X, dY, n, d.ci, Wg, Wu, d.f, Wd, d.co, act, H, dG, dU, ws + L.pack, s);
             } else {
                 hipLaunchKernelGGL(k_ffn_mid_bf16<4>, dim3((unsigned)(ceil_div(n, 128) * nf)), dim3(256), 0, s, x.p, x.ld,
-                                   y.p, y.ld, n, d.ci, d.co, g.p, u.p, g.ld, w.p, w.ld, d.f, act, H, dGU, (int)d.f8, nf);
+                                   y.p, y.ld, n, d.ci, d.co, g.p, u.p, g.ld, w.p, w.ld, d.f, act, H, dG, dU, nf);
             }
-            if (dX) ffn_gemm_kc(dGU, dGU + d.f8, 2 * d.f8, n, d.f, g.p, u.p, g.ld, d.ci, dX, s);
+            if (dX) ffn_gemm_kc(ffn_const(dG), ffn_const(dU), n, d.f, g.p, u.p, g.ld, d.ci, dX, s);
         } else {
-            ffn_bwd_rows(d, L, X, Wg, Wu, Wd, dY, act, dX, ws, s);
+            ffn_bwd_rows(d, X, Wg, Wu, Wd, dY, act, dX, H, dG, dU, s);
         }
     }
     if (!dWg && !dWu && !dWd) return;
     const bool up = dWg || dWu;
-    const DwSide<T> p0{xs, dGU, ldx, 2 * d.f8, d.ci, (int)(2 * d.f8), L.tn0, up ? L.t0 : 0, 0};
-    const DwSide<T> p1{H, ys, d.f8, ldy, d.f, d.co, L.tn1, dWd ? L.t1 : 0, L.up};
+    const DwSide<T> p0{row_major(xs, ldx), ffn_const(dG), d.ci, (int)(2 * d.fp), L.tn0, up ? L.t0 : 0, 0};
+    const DwSide<T> p1{ffn_const(H), row_major(ys, ldy), d.f, d.co, L.tn1, dWd ? L.t1 : 0, L.up};
     if (n > 0) ffn_dw(L, p0, p1, n, part, s);
     const int64_t total = dWd ? L.per_chunk : L.up;
     const int64_t blocks = ceil_div(total, kFfnThreads);
     hipLaunchKernelGGL(k_ffn_dw_sum<T>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kFfnThreads), 0, s, part,
-                       n > 0 ? L.chunks : 0, L.per_chunk, d.ci, d.f, (int)d.f8, d.co, dWg, dWu, dWd, L.up, total);
+                       n > 0 ? L.chunks : 0, L.per_chunk, d.ci, d.f, (int)d.fp, d.co, dWg, dWu, dWd, L.up, total);
 }
 
 }  // namespace gsc

@@ -12,7 +12,8 @@
 //       fragments are 16-byte reads.
 //   MC, the reduction across the rows: a line of 64, 128 or 256 columns per reduction element k, its 32-byte
 //       pairs of pieces permuted by bits of k such that the eight lines which a transpose read
-//       (ds_read_b64_tr_b16) serves together lie in distinct banks.  Within each 16 lanes, lane i of such a
+//       (ds_read_b64_tr_b16) serves together lie in distinct banks; of an operand in blocks (row_blocks) lines
+//       of 32 columns, 32 of them after each other, so that a load takes 1 KiB of a block.  Within each 16 lanes, lane i of such a
 //       read receives element i % 4 of the 8-byte pieces that lanes i / 4, i / 4 + 4, ... address.
 //
 // A step's LDS reads are one block of inline assembly that also waits for them: the compiler cannot tell
@@ -40,26 +41,30 @@ __device__ __forceinline__ void fb_barrier() {
     asm volatile("" ::: "memory");
 }
 
-// One side of a product: element (r, k) at p[r ld + k] (KC) or p[k ld + r] (MC), r < rows, k < the
-// product's reduction length (both whole pieces along the line).
+// One side of a product: element (r, k) at row r and column k of m (KC), or row k and column r (MC), r < rows, k < the
+// product's reduction length (both whole pieces along m's rows).
 struct FbSide {
-    const uint16_t* p;
-    int64_t ld;
+    RowMat<const uint16_t> m;
     int64_t rows;
 };
 
+// How a side lies: the reduction along its rows, across them, or across them in blocks.
+enum FbLay { FB_KC, FB_MC, FB_MB };
+
 // The copies of R rows (columns) of a side by a block of NW waves.
-template <bool MC, int R, int NW>
+template <FbLay LAY, int R, int NW>
 struct FbCopy {
     static constexpr int INS = R / 16;                        // load instructions (1 KiB) of a stage
     static constexpr int N = (INS + NW - 1) / NW;             // ... per wave
     static constexpr int BYTES = R * 64;
-    static constexpr int LINE = R * 2;                        // MC: bytes of a line
-    static constexpr int LPI = 1024 / LINE;                   // MC: lines of an instruction (R <= 512)
+    static constexpr int LINE = LAY == FB_MB ? 64 : R * 2;    // MC, MB: bytes of a line
+    static constexpr int LPI = 1024 / LINE;                   // ... lines of an instruction (R <= 512)
+    static constexpr int HALF = 4 * LINE;                     // ... four lines on: the second half of a transpose read
     static_assert(INS % NW == 0, "waves share a stage's copies evenly");
 
     // permutation of a line's pairs
     static __device__ __forceinline__ int perm(int k) {
+        if (LAY == FB_MB) return (k >> 3) & 1;
         return R == 64 ? ((k >> 1) & 1) | ((k >> 2) & 2) : (k & 3) | ((k >> 1) & 4);
     }
 
@@ -71,24 +76,29 @@ struct FbCopy {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             const int ins = wave * N + j;
-            if (MC) {
-                const int k = ins * LPI + lane / (64 / LPI), slot = lane % (64 / LPI);
-                const int piece = ((((slot >> 1) ^ perm(k)) << 1) | (slot & 1));
-                first[j] = k;
-                off[j] = piece * 8 < s.rows ? (uint32_t)((int64_t)k * s.ld * 2 + piece * 16) : kFbNone;
+            int row, col;   // of m; its piece's first column
+            bool in;
+            if (LAY == FB_KC) {
+                row = ins * 16 + (lane >> 2);
+                col = ((lane & 3) ^ ((lane >> 3) & 3)) * 8;
+                first[j] = col;
+                in = row < s.rows;
             } else {
-                const int row = ins * 16 + (lane >> 2), piece = (lane & 3) ^ ((lane >> 3) & 3);
-                first[j] = piece * 8;
-                off[j] = row < s.rows ? (uint32_t)((int64_t)row * s.ld * 2 + piece * 16) : kFbNone;
+                row = (LAY == FB_MB ? ins % 2 : ins) * LPI + lane / (64 / LPI);
+                const int slot = lane % (64 / LPI);
+                col = ((((slot >> 1) ^ perm(row)) << 1) | (slot & 1)) * 8 + (LAY == FB_MB ? ins / 2 * 32 : 0);
+                first[j] = row;
+                in = col < s.rows;
             }
+            off[j] = in ? (uint32_t)((row >> 7) * s.m.ts + (row & 127) * s.m.ld + (col >> 5) * s.m.gs + (col & 31)) * 2 : kFbNone;
         }
     }
     // the step at reduction element k0 of K, into LDS at dst
     __device__ __forceinline__ void issue(const FbSide& s, int64_t k0, int64_t K, uint8_t* dst, int wave) const {
-        const uint16_t* base = s.p + (MC ? k0 * s.ld : k0);
+        const uint16_t* base = LAY == FB_KC ? s.m.at(0, k0).p : s.m.at(k0, 0).p;
         // an upper bound of the bytes from there on that may be read; what lies outside the operand is masked below
         const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, 0x7fffffff, kFbBufFlags);
-        const int left = (int)(K - k0 < 32 ? K - k0 : 32);
+        const int left = (int)(K - k0 < 32 ? K - k0 : 32);   // (none from K on)
 #pragma unroll
         for (int j = 0; j < N; ++j)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
@@ -206,19 +216,18 @@ __device__ __forceinline__ uint32_t fb_frag_kc() {
     const int i = threadIdx.x & 15, q = (threadIdx.x & 63) >> 4;
     return (uint32_t)(i * 64 + ((q ^ ((i >> 1) & 3)) * 16));
 }
-// lane's byte in an MC stage of R columns for the 16 columns 16 t ..
-template <int R>
+// lane's byte in an MC or MB stage of R columns for the 16 columns 16 t ..
+template <FbLay LAY, int R>
 __device__ __forceinline__ uint32_t fb_frag_mc(int t) {
+    typedef FbCopy<LAY, R, R / 16> C;
     const int i = threadIdx.x & 15, q = (threadIdx.x & 63) >> 4;
     const int k = 8 * q + (i >> 2);
-    return (uint32_t)(k * R * 2 + ((t ^ FbCopy<true, R, R / 16>::perm(k)) * 32) + 8 * (i & 3));
+    if (LAY == FB_MB) return (uint32_t)((t >> 1) * 2048 + k * 64 + (((t & 1) ^ C::perm(k)) * 32) + 8 * (i & 3));
+    return (uint32_t)(k * R * 2 + ((t ^ C::perm(k)) * 32) + 8 * (i & 3));
 }
 
-// What the B side of a product is: rows of the reduction (KC), columns across it (MC), or two MC
-// sides of half as many columns each (PAIR: a wave takes half of its columns from either).
-enum FbB { FB_KC, FB_MC, FB_PAIR };
-
-// acc += A B^T of a block of WM x WN waves, wave tiles of 16 MT rows by 16 NT columns.  The second operand
+// acc += A B^T of a block of WM x WN waves, wave tiles of 16 MT rows by 16 NT columns.  PAIR: B's columns are two sides of
+// half as many each, the second one's rows at b2 (a wave takes half of its columns from either).  The second operand
 // goes into the MFMA first: lane (i, q) gets row 16 mi + i of its rows and four consecutive columns
 // 4 q .. of block ni.  lds: NS stages.  Every wave has passed its last read of lds before the call.
 template <int WM, int WN, int MT, int NT, int NS = 3>
@@ -228,43 +237,43 @@ struct FbShape {
     static constexpr int LDS = NS * STAGE;
 };
 
-template <int WM, int WN, int MT, int NT, bool AMC, FbB BK, int NS = 3>
+template <int WM, int WN, int MT, int NT, FbLay AL, FbLay BL, bool PAIR = false, int NS = 3>
 __device__ __forceinline__ void fb_product(const FbSide& A, const FbSide& B, const uint16_t* b2, int64_t K, uint8_t* lds,
                                            floatx4 (&acc)[MT][NT]) {
     typedef FbShape<WM, WN, MT, NT> S;
-    constexpr int RB = BK == FB_PAIR ? S::BN / 2 : S::BN;
-    typedef FbCopy<AMC, S::BM, S::NW> CA;
-    typedef FbCopy<BK != FB_KC, RB, S::NW> CB;
-    constexpr int LD = CA::N + CB::N * (BK == FB_PAIR ? 2 : 1);
+    constexpr int RB = PAIR ? S::BN / 2 : S::BN;
+    typedef FbCopy<AL, S::BM, S::NW> CA;
+    typedef FbCopy<BL, RB, S::NW> CB;
+    constexpr int LD = CA::N + CB::N * (PAIR ? 2 : 1);
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave / WN, wn = wave % WN;
     CA ca;
     CB cb;
     ca.start(A, wave);
     cb.start(B, wave);
-    const FbSide B2{b2, B.ld, B.rows};
+    const FbSide B2{{b2, B.m.ld, B.m.gs, B.m.ts}, B.rows};
     const int steps = (int)((K + 31) / 32);
     auto issue = [&](int s, int slot) {
         uint8_t* d = lds + slot * S::STAGE;
         ca.issue(A, (int64_t)s * 32, K, d, wave);
         cb.issue(B, (int64_t)s * 32, K, d + CA::BYTES, wave);
-        if (BK == FB_PAIR) cb.issue(B2, (int64_t)s * 32, K, d + CA::BYTES + CB::BYTES, wave);
+        if (PAIR) cb.issue(B2, (int64_t)s * 32, K, d + CA::BYTES + CB::BYTES, wave);
     };
-    uint32_t fa[AMC ? MT : 1], fb[BK == FB_KC ? 1 : 4];
-    if constexpr (AMC) {
+    uint32_t fa[AL == FB_KC ? 1 : MT], fb[BL == FB_KC ? 1 : 4];
+    if constexpr (AL != FB_KC) {
 #pragma unroll
-        for (int t = 0; t < MT; ++t) fa[t] = fb_lds(lds) + fb_frag_mc<S::BM>(MT * wm + t);
+        for (int t = 0; t < MT; ++t) fa[t] = fb_lds(lds) + fb_frag_mc<AL, S::BM>(MT * wm + t);
     } else {
         fa[0] = fb_lds(lds) + fb_frag_kc() + wm * MT * 1024;
     }
-    if constexpr (BK == FB_KC) {
+    if constexpr (BL == FB_KC) {
         fb[0] = fb_lds(lds) + CA::BYTES + fb_frag_kc() + wn * NT * 1024;
-    } else if constexpr (BK == FB_MC) {
+    } else if constexpr (!PAIR) {
 #pragma unroll
-        for (int t = 0; t < NT; ++t) fb[t] = fb_lds(lds) + CA::BYTES + fb_frag_mc<RB>(NT * wn + t);
+        for (int t = 0; t < NT; ++t) fb[t] = fb_lds(lds) + CA::BYTES + fb_frag_mc<BL, RB>(NT * wn + t);
     } else {
 #pragma unroll
         for (int t = 0; t < NT; ++t)
-            fb[t] = fb_lds(lds) + CA::BYTES + (t < NT / 2 ? 0 : CB::BYTES) + fb_frag_mc<RB>(NT / 2 * wn + t % (NT / 2));
+            fb[t] = fb_lds(lds) + CA::BYTES + (t < NT / 2 ? 0 : CB::BYTES) + fb_frag_mc<BL, RB>(NT / 2 * wn + t % (NT / 2));
     }
 #pragma unroll
     for (int s = 0; s < NS - 1; ++s)
@@ -278,19 +287,19 @@ __device__ __forceinline__ void fb_product(const FbSide& A, const FbSide& B, con
         if (s + NS - 1 < steps) issue(s + NS - 1, into);
         fbf16x8 a[MT], b[NT];
         const uint32_t at = (uint32_t)(slot * S::STAGE);
-        if constexpr (BK == FB_KC) {
+        if constexpr (BL == FB_KC) {
             fb_read_kk(fa[0] + at, fb[0] + at, a, b);
         } else {
             uint32_t vb[4];
 #pragma unroll
             for (int t = 0; t < 4; ++t) vb[t] = fb[t] + at;
-            if constexpr (AMC) {
+            if constexpr (AL != FB_KC) {
                 uint32_t va[MT];
 #pragma unroll
                 for (int t = 0; t < MT; ++t) va[t] = fa[t] + at;
-                fb_read_mm<4 * S::BM * 2, 4 * RB * 2>(va, vb, a, b);
+                fb_read_mm<CA::HALF, CB::HALF>(va, vb, a, b);
             } else {
-                fb_read_km<4 * RB * 2>(fa[0] + at, vb, a, b);
+                fb_read_km<CB::HALF>(fa[0] + at, vb, a, b);
             }
         }
 #pragma unroll

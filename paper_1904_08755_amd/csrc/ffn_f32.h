@@ -13,13 +13,12 @@ constexpr int kFfnThreads = 256;
 constexpr int kFfnRowBytes = 128;               // reduction bytes of a step
 constexpr int kFfnBk = kFfnRowBytes / 4;
 
-// One side of a product: `rows` outputs by k reduction elements, element (r, k) at p[r ld + k] (KC)
-// or p[k ld + r] (MC).  Rows and reduction elements behind the end read as 0.  SPLIT: the tile's rows
-// [0, R / 2) come from p and the others from p2 (both from row 0 on).
+// One side of a product: `rows` outputs by k reduction elements, element (r, k) at row r and column k of m (KC) or at
+// row k and column r (MC).  Rows and reduction elements behind the end read as 0.  SPLIT: the tile's rows
+// [0, R / 2) come from m and the others from p2, laid out alike (both from row 0 on).
 struct Side {
-    const float* p;
+    RowMat<const float> m;
     const float* p2;
-    int64_t ld;
     int64_t rows;
     int64_t k;
 };
@@ -33,8 +32,7 @@ struct TileCopy {
     static_assert(N >= 1 && kFfnThreads % PER == 0, "tile");
     typedef RowVec<float>::Raw Raw;
 
-    const float* base;      // element (0, 0) of the thread's side
-    int64_t ld;
+    RowMat<const float> m;  // from element (0, 0) of the thread's side on
     int line, at;       // first row (KC) or reduction element (MC), and the piece's first element across
     int64_t across;     // MC: elements from `at` to the rows' end
     int lim;            // KC: valid lines
@@ -44,20 +42,19 @@ struct TileCopy {
         const int c = threadIdx.x % PER;
         line = threadIdx.x / PER;
         at = c * V;
-        base = s.p;
-        ld = s.ld;
+        m = s.m;
         if (KC) {
             lim = (int)(s.rows < R ? s.rows : R);
             across = 0;
         } else {
             int col = at;
             if (SPLIT && at >= R / 2) {
-                base = s.p2;
+                m.p = s.p2;
                 col -= R / 2;
             }
             across = s.rows - col;
             if (SPLIT && across > R / 2 - col) across = R / 2 - col;
-            base += col;
+            m.p += (col >> 5) * m.gs + (col & 31);
             lim = 0;
         }
     }
@@ -65,20 +62,20 @@ struct TileCopy {
     __device__ __forceinline__ void fetch(int64_t k0, int64_t k) {
         constexpr int DL = kFfnThreads / PER;   // lines between a thread's pieces
         if (KC) {
-            const float* b = base + k0 + at;
+            const float* b = m.p + (k0 >> 5) * m.gs + at;
             const int64_t left = k - k0 - at;
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const int row = line + j * DL;
-                r[j] = load_vec<float, true>(b + (int64_t)row * ld, row < lim ? left : 0);
+                r[j] = load_vec<float, true>(b + (int64_t)row * m.ld, row < lim ? left : 0);
             }
         } else {
-            const float* b = base + k0 * ld;
+            const float* b = m.p + (k0 >> 7) * m.ts + (k0 & 127) * m.ld;
             const int kl = (int)(k - k0 < BK ? k - k0 : BK);
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 const int kk = line + j * DL;
-                r[j] = load_vec<float, true>(b + (int64_t)kk * ld, kk < kl ? across : 0);
+                r[j] = load_vec<float, true>(b + (int64_t)kk * m.ld, kk < kl ? across : 0);
             }
         }
     }

@@ -1,7 +1,7 @@
 // Feed-forward kernels for many rows of at most 256 channels on either side (bfloat16; ffn_res.hip), used by ffn.hip.
 #pragma once
 
-#include "gsc_internal.h"
+#include "row_vec.h"
 
 namespace gsc {
 
@@ -14,8 +14,9 @@ size_t res_pack_bytes(int ci, int f, int co, bool bwd);
 void res_fwd(const uint16_t* X, int64_t n, int ci, const uint16_t* Wg, const uint16_t* Wu, int f, const uint16_t* Wd, int co,
              int act, uint16_t* Y, void* pack, hipStream_t s);
 
-// H (n x f8, f8 = f in whole eights, zeros behind f) and dG, dU (side by side, n x 2 f8).
+// H, dG and dU (row_blocks; columns behind f up to whole 64s zero).
 void res_mid(const uint16_t* X, const uint16_t* dY, int64_t n, int ci, const uint16_t* Wg, const uint16_t* Wu, int f,
-             const uint16_t* Wd, int co, int act, uint16_t* H, uint16_t* dGU, int64_t f8, void* pack, hipStream_t s);
+             const uint16_t* Wd, int co, int act, RowMat<uint16_t> H, RowMat<uint16_t> dG, RowMat<uint16_t> dU, void* pack,
+             hipStream_t s);
 
 }  // namespace gsc

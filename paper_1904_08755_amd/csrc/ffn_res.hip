@@ -122,29 +122,28 @@ struct ResCopies {
     int pairs, lasts;             // left of either kind
     int wave;
 
-    // starts stage S (a number of the order; beyond the end nothing)
+    // Starts stage S (a number of the order).  Copies that carry nothing are started beyond the end, so that the number in
+    // flight is the same everywhere: with branches around them the compiler cannot tell which have landed and waits for all
+    // of them before it reads a stage.
     template <int S>
     __device__ __forceinline__ void start(uint8_t* dst) {
         constexpr int L = O::loads(S);
         int& left = O::last(S) ? lasts : pairs;
         const uint8_t*& src = O::last(S) ? last : pair;
-        if (left <= 0) return;
-        --left;
         const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)src, (short)0, 0x7fffffff, kFbBufFlags);
-        const uint32_t off = (uint32_t)(wave * L * 1024 + (threadIdx.x & 63) * 16);
+        const uint32_t off = left > 0 ? (uint32_t)(wave * L * 1024 + (threadIdx.x & 63) * 16) : kFbNone;
 #pragma unroll
         for (int j = 0; j < L; ++j)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 rs, (__attribute__((address_space(3))) void*)(dst + (wave * L + j) * 1024), 16, off + j * 1024, 0, 0, 0);
+        --left;
         src += L * 8192;
     }
     // Until stage S has landed for all waves.  MORE: memory instructions of this wave since, other than copies (they retire in
-    // order); `end`: near the end, where not all later stages exist.  Every wave's LDS reads and writes before it are
-    // done, so what they read may be written again.
+    // order).  Every wave's LDS reads and writes before it are done, so what they read may be written again.
     template <int S, int MORE>
-    __device__ __forceinline__ void wait(bool end) {
-        if (end) fb_wait<0>();
-        else fb_wait<O::later(S) + MORE>();
+    __device__ __forceinline__ void wait() {
+        fb_wait<O::later(S) + MORE>();
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
         fb_barrier();
     }
@@ -164,13 +163,13 @@ struct ResPairFrag {
     fbf16x8 a, b;
 };
 
-// H (n x f8) and dG, dU (n x 2 f8) of 128 rows and `per` hidden chunks from blockIdx.y * per on.  KT: 16-element steps of the
+// H, dG and dU of 128 rows and `per` hidden chunks from blockIdx.y * per on.  KT: 16-element steps of the
 // wider of ci and co (4, 8 or 16); W: the weights packed for it.  The block's dY lies in LDS as fragments (the registers
 // hold X, a chunk's sums and those of the chunk before).
 template <int KT, int ACT>
 __global__ void __launch_bounds__(kResThreads, 1)
 k_ffn_mid_res(const uint16_t* __restrict__ X, const uint16_t* __restrict__ dY, int64_t n, int ci, int co,
-              const uint8_t* __restrict__ W, int f, uint16_t* __restrict__ H, uint16_t* __restrict__ dGU, int64_t f8, int per) {
+              const uint8_t* __restrict__ W, int f, RowMat<uint16_t> H, RowMat<uint16_t> dG, RowMat<uint16_t> dU, int per) {
     typedef ResOrder<KT, 0> O;
     RES_SLOTS(O)
     __shared__ __attribute__((aligned(1024))) uint8_t dys[4 * KT * 1024];
@@ -193,7 +192,6 @@ k_ffn_mid_res(const uint16_t* __restrict__ X, const uint16_t* __restrict__ dY, i
         for (int k = 0; k < KT / 2; ++k)
             *reinterpret_cast<fbf16x8*>(dyw + (wn * (KT / 2) + k) * 1024 + (threadIdx.x & 63) * 16) = d[k];
     }
-    const bool whole = r0 + 32 <= n;
     res_each<O::SLOTS - 1>([&](auto N) { cp.template start<decltype(N)::value>(slot(N)); });
     floatx16 pg{}, pu{}, pd{};   // the chunk before: gates, partners and dH, then dG, dU and H
     uint32_t ph[8];
@@ -207,56 +205,63 @@ k_ffn_mid_res(const uint16_t* __restrict__ X, const uint16_t* __restrict__ dY, i
     };
     // array k of the chunk before, as bfloat16 pairs
     auto put = [&](int k, int ch, bool in) {
-        const int64_t col = (int64_t)(ch0 + ch) * 64 + 32 * wn;
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             ph[e] = k == 0 ? pack_bf16(pd[2 * e], pd[2 * e + 1])
                            : (k == 1 ? pack_bf16(pg[2 * e], pg[2 * e + 1]) : pack_bf16(pu[2 * e], pu[2 * e + 1]));
-        uint16_t* out = k == 0 ? H : (k == 1 ? dGU : dGU + f8);
-        const int64_t ld = k == 0 ? f8 : 2 * f8;
-        if (in) res_store<true>(out, ld, r0, n, col, f8, ph);
-        else res_store<false>(out, ld, r0, n, col, f8, ph);
+        // the wave's 32 rows of a block of 128 rows by 32 columns
+        uint16_t* out = (k == 0 ? H : (k == 1 ? dG : dU)).at(r0, (int64_t)(ch0 + ch) * 64 + 32 * wn).p;
+        if (in) res_store<true>(out, 32, 0, n - r0, 0, 32, ph);
+        else res_store<false>(out, 32, 0, n - r0, 0, 32, ph);
     };
-    for (int cb = 0; cb < chunks; cb += O::U)
-        res_each<O::U>([&](auto UU) {
-            constexpr int u = decltype(UU)::value;
-            const int ch = cb + u;
-            if (ch >= chunks) return;
-            const bool end = ch + 3 >= chunks || !whole;   // (not whole: the number of stores is not known)
-            const bool first = ch < 2;                      // no stores yet
-            floatx16 g{}, up{}, dh{};
-            res_each<O::PS>([&](auto P) {
-                constexpr int p = decltype(P)::value, S = u * O::SPC + p, E = 16 / O::PS / (2 * O::KP / 4);
-                if (first) cp.template wait<S, 0>(end);
-                else cp.template wait<S, 6>(end);
+    // WHOLE: all of the wave's rows exist, and six stores follow the start of every chunk's last stage, so that the waits can
+    // count them (before the first chunk, and in it, they write zeros where its values come later).
+    auto run = [&](auto WHOLE) {
+        constexpr bool in = decltype(WHOLE)::value;
+        if (in) {
+#pragma unroll
+            for (int k = 0; k < 3; ++k) put(k, 0, true);
+        }
+        for (int cb = 0; cb < chunks; cb += O::U)
+            res_each<O::U>([&](auto UU) {
+                constexpr int u = decltype(UU)::value;
+                const int ch = cb + u;
+                if (ch >= chunks) return;
+                floatx16 g{}, up{}, dh{};
+                res_each<O::PS>([&](auto P) {
+                    constexpr int p = decltype(P)::value, S = u * O::SPC + p, E = 16 / O::PS / (2 * O::KP / 4);
+                    cp.template wait<S, in ? 6 : 0>();
+                    cp.template start<S + O::SLOTS - 1>(slot(std::integral_constant<int, S + O::SLOTS - 1>{}));
+                    const uint8_t* b = slot(std::integral_constant<int, S>{}) + wn * 2048;
+                    res_stream<2 * O::KP, 4, 7>(
+                        [&](int j) { return res_frag(b + (j >> 1) * 4096 + (j & 1) * 1024); },
+                        [&](int j, fbf16x8 w) {
+                            if (j & 1) up = res_mma(w, x[p * O::KP + (j >> 1)], up);
+                            else g = res_mma(w, x[p * O::KP + (j >> 1)], g);
+                        },
+                        [&](auto I) {
+#pragma unroll
+                            for (int e = 0; e < E; ++e) epi(p * (16 / O::PS) + decltype(I)::value * E + e);
+                        });
+                });
+                constexpr int S = u * O::SPC + O::PS;
+                cp.template wait<S, in && O::PS == 1 ? 6 : 0>();
                 cp.template start<S + O::SLOTS - 1>(slot(std::integral_constant<int, S + O::SLOTS - 1>{}));
-                const uint8_t* b = slot(std::integral_constant<int, S>{}) + wn * 2048;
-                res_stream<2 * O::KP, 4, 7>(
-                    [&](int j) { return res_frag(b + (j >> 1) * 4096 + (j & 1) * 1024); },
-                    [&](int j, fbf16x8 w) {
-                        if (j & 1) up = res_mma(w, x[p * O::KP + (j >> 1)], up);
-                        else g = res_mma(w, x[p * O::KP + (j >> 1)], g);
-                    },
-                    [&](auto I) {
+                const uint8_t* b = slot(std::integral_constant<int, S>{}) + wn * 1024;
+                if (in || ch > 0) {
 #pragma unroll
-                        for (int e = 0; e < E; ++e) epi(p * (16 / O::PS) + decltype(I)::value * E + e);
-                    });
+                    for (int k = 0; k < 3; ++k) put(k, ch > 0 ? ch - 1 : 0, in);
+                }
+                res_stream<KT, 4, 0>([&](int j) { return ResPairFrag{res_frag(b + j * 2048), res_frag(dyw + j * 1024)}; },
+                                     [&](int j, const ResPairFrag& w) { dh = res_mma(w.a, w.b, dh); }, [](auto) {});
+                pg = g;
+                pu = up;
+                pd = dh;
             });
-            constexpr int S = u * O::SPC + O::PS;
-            if (first || O::PS > 1) cp.template wait<S, 0>(end);
-            else cp.template wait<S, 6>(end);   // (the stores came after this stage's start)
-            cp.template start<S + O::SLOTS - 1>(slot(std::integral_constant<int, S + O::SLOTS - 1>{}));
-            const uint8_t* b = slot(std::integral_constant<int, S>{}) + wn * 1024;
-            if (ch > 0) {
-#pragma unroll
-                for (int k = 0; k < 3; ++k) put(k, ch - 1, whole);
-            }
-            res_stream<KT, 4, 0>([&](int j) { return ResPairFrag{res_frag(b + j * 2048), res_frag(dyw + j * 1024)}; },
-                                 [&](int j, const ResPairFrag& w) { dh = res_mma(w.a, w.b, dh); }, [](auto) {});
-            pg = g;
-            pu = up;
-            pd = dh;
-        });
+    };
+    if (r0 + 32 <= n) run(std::true_type{});
+    else run(std::false_type{});
+    fb_wait<0>();   // no copy is in flight when the block ends
 #pragma unroll
     for (int e = 0; e < 16; ++e) epi(e);
 #pragma unroll
@@ -300,9 +305,9 @@ k_ffn_fwd_res(const uint16_t* __restrict__ X, int64_t n, int ci, int co, const u
                 uint2{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
     };
     // stage S: projections p of a chunk, with a share of the activation of the chunk before
-    auto pairs = [&](auto SS, auto P, bool more, bool end, auto side) {
+    auto pairs = [&](auto SS, auto P, bool more, auto side) {
         constexpr int S = decltype(SS)::value, p = decltype(P)::value;
-        cp.template wait<S, 0>(end);
+        cp.template wait<S, 0>();
         cp.template start<S + O::SLOTS - 1>(slot(std::integral_constant<int, S + O::SLOTS - 1>{}));
         const uint8_t* b = slot(std::integral_constant<int, S>{}) + wn * 2048;
         if (more)
@@ -316,26 +321,26 @@ k_ffn_fwd_res(const uint16_t* __restrict__ X, int64_t n, int ci, int co, const u
         else
             res_each<2 * O::KP / 4>(side);
     };
-    res_each<O::PS>([&](auto P) { pairs(P, P, true, true, [](auto) {}); });
+    res_each<O::PS>([&](auto P) { pairs(P, P, true, [](auto) {}); });
     for (int cb = 0; cb < chunks; cb += O::U)
         res_each<O::U>([&](auto UU) {
             constexpr int u = decltype(UU)::value, S0 = O::PS + u * O::SPC;
             const int ch = cb + u;
             if (ch >= chunks) return;
-            const bool more = ch + 1 < chunks, end = ch + 4 >= chunks;
+            const bool more = ch + 1 < chunks;
             pg = g;
             pu = up;
             g = floatx16{};
             up = floatx16{};
             res_each<O::PS>([&](auto P) {
                 constexpr int p = decltype(P)::value, E = 16 / O::PS / (2 * O::KP / 4);
-                pairs(std::integral_constant<int, S0 + p>{}, P, more, end, [&](auto I) {
+                pairs(std::integral_constant<int, S0 + p>{}, P, more, [&](auto I) {
 #pragma unroll
                     for (int e = 0; e < E; ++e) epi(p * (16 / O::PS) + decltype(I)::value * E + e);
                 });
             });
             constexpr int S = S0 + O::PS;
-            cp.template wait<S, 0>(end);
+            cp.template wait<S, 0>();
             cp.template start<S + O::SLOTS - 1>(slot(std::integral_constant<int, S + O::SLOTS - 1>{}));
             const uint8_t* b = slot(std::integral_constant<int, S>{}) + wn * TW * 1024;
             fbf16x8 a[4];
@@ -345,6 +350,7 @@ k_ffn_fwd_res(const uint16_t* __restrict__ X, int64_t n, int ci, int co, const u
             res_stream<4 * TW, 4, 0>([&](int j) { return res_frag(b + (j / TW * TT + j % TW) * 1024); },
                                      [&](int j, fbf16x8 w) { y[j % TW] = res_mma(w, a[j / TW], y[j % TW]); }, [](auto) {});
         });
+    fb_wait<0>();   // no copy is in flight when the block ends
 #pragma unroll
     for (int t = 0; t < TW; ++t) {
         uint32_t o[8];
@@ -402,14 +408,15 @@ void res_fwd(const uint16_t* X, int64_t n, int ci, const uint16_t* Wg, const uin
 
 // Hidden chunks are split over blocks where the row tiles are fewer than two a compute unit.
 void res_mid(const uint16_t* X, const uint16_t* dY, int64_t n, int ci, const uint16_t* Wg, const uint16_t* Wu, int f,
-             const uint16_t* Wd, int co, int act, uint16_t* H, uint16_t* dGU, int64_t f8, void* pack, hipStream_t s) {
+             const uint16_t* Wd, int co, int act, RowMat<uint16_t> H, RowMat<uint16_t> dG, RowMat<uint16_t> dU, void* pack,
+             hipStream_t s) {
     const int64_t tiles = (n + kResRows - 1) / kResRows, chunks = (f + 63) / 64;
     const int64_t parts = tiles >= 512 ? 1 : (512 + tiles - 1) / tiles;
     const int per = (int)((chunks + parts - 1) / parts);
     res_with(res_pack(ci, f, co, Wg, Wu, Wd, 1, pack, s), act, [&](auto KT, auto ACT) {
         auto* kern = k_ffn_mid_res<decltype(KT)::value, decltype(ACT)::value>;
         hipLaunchKernelGGL(kern, dim3((unsigned)tiles, (unsigned)((chunks + per - 1) / per)), dim3(kResThreads), 0, s, X, dY, n,
-                           ci, co, reinterpret_cast<const uint8_t*>(pack), f, H, dGU, f8, per);
+                           ci, co, reinterpret_cast<const uint8_t*>(pack), f, H, dG, dU, per);
     });
 }
 

@@ -75,4 +75,27 @@ __device__ __forceinline__ void store_vec(T* p, int64_t left, const float (&v)[R
     }
 }
 
+// A matrix as row-major rows of ld elements, or in blocks of 128 rows by 32 columns, each one piece of memory (row-major
+// inside), the blocks of 128 rows after each other: a step of 32 columns of a tile's rows is then contiguous, where a
+// row-major one takes a piece of every row, a power of two apart for the usual widths, and most memory channels idle.
+// Element (r, c) at p[(r / 128) ts + (r % 128) ld + (c / 32) gs + c % 32].
+template <typename T>
+struct RowMat {
+    T* p;
+    int64_t ld, gs, ts;
+    // from row r (a multiple of the rows a tile takes) and column c (a multiple of 32) on
+    __host__ __device__ __forceinline__ RowMat at(int64_t r, int64_t c) const {
+        return {p + (r >> 7) * ts + (r & 127) * ld + (c >> 5) * gs, ld, gs, ts};
+    }
+};
+template <typename T>
+__host__ __device__ __forceinline__ RowMat<T> row_major(T* p, int64_t ld) {
+    return {p, ld, 32, 128 * ld};
+}
+// columns: of all matrices that share the blocks of 128 rows
+template <typename T>
+__host__ __device__ __forceinline__ RowMat<T> row_blocks(T* p, int64_t columns) {
+    return {p, 32, 4096, columns * 128};
+}
+
 }  // namespace gsc
