@@ -321,8 +321,8 @@ __global__ void __launch_bounds__(512, 1)
 k_ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, int64_t k, const uint16_t* __restrict__ B1,
               const uint16_t* __restrict__ B2, int64_t ldb, int co, uint16_t* __restrict__ Out, int nc) {
     constexpr int BN = 64 * TN, STAGE = (256 + BN) * 64;
-    typedef FbCopy<FB_KC, 256, 8> CA;
-    typedef FbCopy<FB_KC, BN, 8> CB;
+    typedef FbCopy<FB_KC, 256, 8, true> CA;
+    typedef FbCopy<FB_KC, BN, 8, true> CB;
     constexpr int LD = CA::N + CB::N;
     __shared__ __attribute__((aligned(1024))) uint8_t slot0[STAGE];
     __shared__ __attribute__((aligned(1024))) uint8_t slot1[STAGE];
@@ -350,7 +350,7 @@ k_ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, i
         cb.issue(second ? b2 : b1, k0, k, dst + CA::BYTES, wave);
     };
     const int i = threadIdx.x & 31, h = (threadIdx.x & 63) >> 5;
-    const int at = i * 64 + ((h ^ ((i >> 1) & 3)) * 16);   // elements 8 h .. of row i; 16 + 8 h .. at ^ 32
+    const int at = i * 64 + ((h ^ ((i >> 2) & 3)) * 16);   // elements 8 h .. of row i; 16 + 8 h .. at ^ 32
     floatx16 acc[2][TN];
 #pragma unroll
     for (int a = 0; a < 2; ++a)

@@ -8,8 +8,8 @@
 // must be whole pieces at 16-byte addresses.
 //
 // Layouts of a stage (a load writes lane after lane, so the permutation is applied to the piece each lane fetches):
-//   KC, the reduction along the rows: rows of 64 bytes, piece c of row r at (c ^ ((r >> 1) & 3)) * 16;
-//       fragments are 16-byte reads.
+//   KC, the reduction along the rows: rows of 64 bytes, piece c of row r at (c ^ ((r >> 1) & 3)) * 16, for
+//       operands of 32 rows at (c ^ ((r >> 2) & 3)) * 16; fragments are 16-byte reads.
 //   MC, the reduction across the rows: a line of 64, 128 or 256 columns per reduction element k, its 32-byte
 //       pairs of pieces permuted by bits of k such that the eight lines which a transpose read
 //       (ds_read_b64_tr_b16) serves together lie in distinct banks; of an operand in blocks (row_blocks) lines
@@ -52,7 +52,8 @@ struct FbSide {
 enum FbLay { FB_KC, FB_MC, FB_MB };
 
 // The copies of R rows (columns) of a side by a block of NW waves.
-template <FbLay LAY, int R, int NW>
+// T32: KC operands of 32 x 32 tiles.
+template <FbLay LAY, int R, int NW, bool T32 = false>
 struct FbCopy {
     static constexpr int INS = R / 16;                        // load instructions (1 KiB) of a stage
     static constexpr int N = (INS + NW - 1) / NW;             // ... per wave
@@ -80,7 +81,7 @@ struct FbCopy {
             bool in;
             if (LAY == FB_KC) {
                 row = ins * 16 + (lane >> 2);
-                col = ((lane & 3) ^ ((lane >> 3) & 3)) * 8;
+                col = ((lane & 3) ^ ((lane >> (T32 ? 4 : 3)) & 3)) * 8;
                 first[j] = col;
                 in = row < s.rows;
             } else {
