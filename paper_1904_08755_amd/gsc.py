@@ -730,28 +730,47 @@ GATES = {"silu": GSC_GATE_SILU, "gelu": GSC_GATE_GELU, "gelu_tanh": GSC_GATE_GEL
 def _fresh(stream):
     """Context in which the buffers of a call on ``stream`` are allocated: they belong to that stream, so neither
     their reuse nor their earlier owners run beside it."""
-    return contextlib.nullcontext() if stream is None else torch.cuda.stream(stream)
+    return _NO_CONTEXT if stream is None else torch.cuda.stream(stream)
 
 
-def _here(X: torch.Tensor, **others):
-    """All tensors of a call (None: not given) lie on X's device, which is the current one (the stream's)."""
-    if X.device.index != torch.cuda.current_device():
+_NO_CONTEXT = contextlib.nullcontext()
+# (the public torch.cuda.current_stream builds a Stream object: 2.4 us of a call that takes 6)
+_current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
+
+
+def _raw_stream(stream, device: int) -> int:
+    if stream is not None:
+        return stream.cuda_stream
+    return torch.cuda.current_stream(device).cuda_stream if _current_raw is None else _current_raw(device)
+
+
+def _addr(t: Optional[torch.Tensor]):
+    return None if t is None else t.data_ptr()
+
+
+def _like(t, shape, dtype, name):
+    """``t`` is a contiguous device tensor of this shape and dtype."""
+    if isinstance(t, torch.Tensor) and t.is_cuda and t.dtype == dtype and t.shape == shape and t.is_contiguous():
+        return
+    _need(t, dtype, name, len(shape))
+    raise ValueError(f"{name} must have shape {tuple(shape)}, got {tuple(t.shape)}")
+
+
+def _here(X: torch.Tensor, *others) -> int:
+    """The device of all tensors of a call (None: not given), which must be the current one (the stream's)."""
+    dev = X.get_device()
+    if dev != torch.cuda.current_device():
         raise ValueError(f"X is on {X.device}, the current device is cuda:{torch.cuda.current_device()}")
-    for name, t in others.items():
-        if t is not None and t.device != X.device:
-            raise ValueError(f"{name} must be on {X.device}, got {t.device}")
+    for t in others:
+        if t is not None and t.get_device() != dev:
+            raise ValueError(f"all tensors must be on {X.device}, got one on {t.device}")
+    return dev
 
 
 def _choice(table, key, name):
     if key not in table:
         raise ValueError(f"{name} must be one of {sorted(table)}, got {key!r}")
     return table[key]
-
-
-def _like(t, ref, dtype, name, dims=2):
-    _need(t, dtype, name, dims)
-    if tuple(t.shape) != tuple(ref):
-        raise ValueError(f"{name} must have shape {tuple(ref)}, got {tuple(t.shape)}")
 
 
 def gsc_layer_norm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor] = None, beta: Optional[torch.Tensor] = None,
@@ -761,19 +780,22 @@ def gsc_layer_norm_fwd(X: torch.Tensor, gamma: Optional[torch.Tensor] = None, be
     dt = _dt(X)
     _need(X, X.dtype, "X", 2)
     n, c = X.shape
-    for name, v in (("gamma", gamma), ("beta", beta)):
-        if v is not None:
-            _like(v, (c,), torch.float32, name, 1)
+    if gamma is not None:
+        _like(gamma, (c,), torch.float32, "gamma")
+    if beta is not None:
+        _like(beta, (c,), torch.float32, "beta")
     if Y is not None:
         _like(Y, X.shape, X.dtype, "Y")
-    _here(X, gamma=gamma, beta=beta, Y=Y)
+    dev = _here(X, gamma, beta, Y)
+    mean = rstd = None
     with _fresh(stream):
         if Y is None:
             Y = torch.empty_like(X)
-        st = torch.empty((2, n), dtype=torch.float32, device=X.device) if stats else (None, None)
-    _check(lib().gsc_layer_norm_fwd(dt, _ptr(X), n, c, _ptr(gamma), _ptr(beta), eps, _ptr(Y), _ptr(st[0]), _ptr(st[1]),
-                                    _stream(stream)))
-    return Y, st[0], st[1]
+        if stats:
+            mean, rstd = torch.empty((2, n), dtype=torch.float32, device=X.device).unbind(0)
+    _check(lib().gsc_layer_norm_fwd(dt, X.data_ptr(), n, c, _addr(gamma), _addr(beta), eps, Y.data_ptr(), _addr(mean),
+                                    _addr(rstd), _raw_stream(stream, dev)))
+    return Y, mean, rstd
 
 
 def gsc_layer_norm_bwd(X: torch.Tensor, dY: torch.Tensor, mean: torch.Tensor, rstd: torch.Tensor,
@@ -785,39 +807,43 @@ def gsc_layer_norm_bwd(X: torch.Tensor, dY: torch.Tensor, mean: torch.Tensor, rs
     _need(X, X.dtype, "X", 2)
     n, c = X.shape
     _like(dY, X.shape, X.dtype, "dY")
-    _like(mean, (n,), torch.float32, "mean", 1)
-    _like(rstd, (n,), torch.float32, "rstd", 1)
+    _like(mean, (n,), torch.float32, "mean")
+    _like(rstd, (n,), torch.float32, "rstd")
     if gamma is not None:
-        _like(gamma, (c,), torch.float32, "gamma", 1)
+        _like(gamma, (c,), torch.float32, "gamma")
     if dX is not None:
         _like(dX, X.shape, X.dtype, "dX")
     if ws is not None:
         _need(ws, torch.uint8, "ws", 1)
-    _here(X, dY=dY, mean=mean, rstd=rstd, gamma=gamma, dX=dX, ws=ws)
+    dev = _here(X, dY, mean, rstd, gamma, dX, ws)
+    dgamma = dbeta = None
     with _fresh(stream):
         if need_dx and dX is None:
             dX = torch.empty_like(X)
-        sums = torch.empty((2, c), dtype=torch.float32, device=X.device) if need_sums else (None, None)
-        if need_sums and ws is None:
-            ws = _ws(lib().gsc_layer_norm_bwd_ws_bytes(n, c), X.device)
-    _check(lib().gsc_layer_norm_bwd(dt, _ptr(X), _ptr(dY), n, c, _ptr(gamma), _ptr(mean), _ptr(rstd),
-                                    _ptr(dX) if need_dx else None, _ptr(sums[0]), _ptr(sums[1]),
-                                    _ptr(ws) if need_sums else None, ws.numel() if need_sums else 0, _stream(stream)))
-    return (dX if need_dx else None), sums[0], sums[1]
+        if need_sums:
+            dgamma, dbeta = torch.empty((2, c), dtype=torch.float32, device=X.device).unbind(0)
+            if ws is None:
+                ws = _ws(lib().gsc_layer_norm_bwd_ws_bytes(n, c), X.device)
+    _check(lib().gsc_layer_norm_bwd(dt, X.data_ptr(), dY.data_ptr(), n, c, _addr(gamma), mean.data_ptr(), rstd.data_ptr(),
+                                    dX.data_ptr() if need_dx else None, _addr(dgamma), _addr(dbeta),
+                                    ws.data_ptr() if need_sums else None, ws.numel() if need_sums else 0,
+                                    _raw_stream(stream, dev)))
+    return (dX if need_dx else None), dgamma, dbeta
 
 
 def _heads(t: torch.Tensor, name: str) -> int:
     """Row stride of n x heads x d rows whose heads lie next to each other."""
-    if not isinstance(t, torch.Tensor) or t.device.type != "cuda":
+    if not isinstance(t, torch.Tensor) or not t.is_cuda:
         raise ValueError(f"{name} must be a CUDA (HIP) tensor")
     if t.dim() != 3:
         raise ValueError(f"{name} must have 3 dims (rows, heads, channels)")
     n, H, d = t.shape
-    if (d > 1 and t.stride(2) != 1) or (H > 1 and t.stride(1) != d):
+    ld, sh, sd = t.stride()
+    if (d > 1 and sd != 1) or (H > 1 and sh != d):
         raise ValueError(f"{name}'s heads must lie next to each other in a row")
-    if n > 1 and t.stride(0) < H * d:
+    if n > 1 and ld < H * d:
         raise ValueError(f"{name}'s rows overlap")
-    return t.stride(0) if n > 1 else H * d
+    return ld if n > 1 else H * d
 
 
 def gsc_rotary(X: torch.Tensor, coords: torch.Tensor, axis_pairs: Sequence[int],
@@ -837,30 +863,32 @@ def gsc_rotary(X: torch.Tensor, coords: torch.Tensor, axis_pairs: Sequence[int],
         raise ValueError(f"axis_pairs and scale need {D} entries")
     if Y is not None and (Y.shape != X.shape or Y.dtype != X.dtype):
         raise ValueError("Y must have X's shape and dtype")
-    _here(X, coords=coords, Y=Y)
+    dev = _here(X, coords, Y)
     pm = _choice(ROTARY_PAIRINGS, pairing, "pairing")
     if Y is None:
         with _fresh(stream):
             Y = torch.empty((n, H, d), dtype=X.dtype, device=X.device)
-    ldy = _heads(Y, "Y")
-    sc = None if scale is None else (ctypes.c_double * max(D, 1))(*[float(v) for v in scale])
-    _check(lib().gsc_rotary(dt, _ptr(X), n, H, d, ldx, _ptr(coords), D,
-                            (ctypes.c_int32 * max(D, 1))(*[int(v) for v in axis_pairs]), sc, float(base), pm,
-                            1 if inverse else 0, _ptr(Y), ldy, _stream(stream)))
+        ldy = H * d
+    else:
+        ldy = _heads(Y, "Y")
+    D_ = max(D, 1)   # (D = 0 is refused by the library)
+    sc = None if scale is None else (ctypes.c_double * D_)(*scale)
+    _check(lib().gsc_rotary(dt, X.data_ptr(), n, H, d, ldx, coords.data_ptr(), D, (ctypes.c_int32 * D_)(*axis_pairs), sc,
+                            base, pm, 1 if inverse else 0, Y.data_ptr(), ldy, _raw_stream(stream, dev)))
     return Y
 
 
 def _ffn_args(X, Wg, Wu, Wd, act):
     dt = _dt(X)
     _need(X, X.dtype, "X", 2)
-    n, ci = X.shape
     _need(Wg, X.dtype, "Wg", 2)
-    f = Wg.shape[1]
+    _need(Wd, X.dtype, "Wd", 2)
+    n, ci = X.shape
+    f, co = Wg.shape[1], Wd.shape[1]
     _like(Wg, (ci, f), X.dtype, "Wg")
     _like(Wu, (ci, f), X.dtype, "Wu")
-    _need(Wd, X.dtype, "Wd", 2)
-    _like(Wd, (f, Wd.shape[1]), X.dtype, "Wd")
-    return dt, n, ci, f, Wd.shape[1], _choice(GATES, act, "act")
+    _like(Wd, (f, co), X.dtype, "Wd")
+    return dt, n, ci, f, co, _choice(GATES, act, "act")
 
 
 def gsc_gated_ffn_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: torch.Tensor, act: str = "silu",
@@ -871,14 +899,14 @@ def gsc_gated_ffn_fwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: t
         _like(Y, (n, co), X.dtype, "Y")
     if ws is not None:
         _need(ws, torch.uint8, "ws", 1)
-    _here(X, Wg=Wg, Wu=Wu, Wd=Wd, Y=Y, ws=ws)
+    dev = _here(X, Wg, Wu, Wd, Y, ws)
     with _fresh(stream):
         if Y is None:
             Y = torch.empty((n, co), dtype=X.dtype, device=X.device)
         if ws is None:
             ws = _ws(lib().gsc_gated_ffn_fwd_ws_bytes(dt, n, ci, f, co), X.device)
-    _check(lib().gsc_gated_ffn_fwd(dt, _ptr(X), n, ci, _ptr(Wg), _ptr(Wu), f, _ptr(Wd), co, gate, _ptr(Y), _ptr(ws),
-                                   ws.numel(), _stream(stream)))
+    _check(lib().gsc_gated_ffn_fwd(dt, X.data_ptr(), n, ci, Wg.data_ptr(), Wu.data_ptr(), f, Wd.data_ptr(), co, gate,
+                                   Y.data_ptr(), ws.data_ptr(), ws.numel(), _raw_stream(stream, dev)))
     return Y
 
 
@@ -893,14 +921,16 @@ def gsc_gated_ffn_bwd(X: torch.Tensor, Wg: torch.Tensor, Wu: torch.Tensor, Wd: t
         _like(dX, X.shape, X.dtype, "dX")
     if ws is not None:
         _need(ws, torch.uint8, "ws", 1)
-    _here(X, Wg=Wg, Wu=Wu, Wd=Wd, dY=dY, dX=dX, ws=ws)
+    dev = _here(X, Wg, Wu, Wd, dY, dX, ws)
+    dW = [None] * 3
     with _fresh(stream):
         if need_dx and dX is None:
             dX = torch.empty_like(X)
-        dW = [torch.empty_like(W) if need_dw else None for W in (Wg, Wu, Wd)]
+        if need_dw:
+            dW = [torch.empty_like(W) for W in (Wg, Wu, Wd)]
         if ws is None:
             ws = _ws(lib().gsc_gated_ffn_bwd_ws_bytes(dt, n, ci, f, co), X.device)
-    _check(lib().gsc_gated_ffn_bwd(dt, _ptr(X), n, ci, _ptr(Wg), _ptr(Wu), f, _ptr(Wd), co, _ptr(dY), gate,
-                                   _ptr(dX) if need_dx else None, *[_ptr(W) for W in dW], _ptr(ws), ws.numel(),
-                                   _stream(stream)))
+    _check(lib().gsc_gated_ffn_bwd(dt, X.data_ptr(), n, ci, Wg.data_ptr(), Wu.data_ptr(), f, Wd.data_ptr(), co,
+                                   dY.data_ptr(), gate, dX.data_ptr() if need_dx else None, *[_addr(W) for W in dW],
+                                   ws.data_ptr(), ws.numel(), _raw_stream(stream, dev)))
     return (dX if need_dx else None), *dW
