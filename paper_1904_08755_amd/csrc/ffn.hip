@@ -496,29 +496,52 @@ k_ffn_dw_sum(const float* __restrict__ part, int64_t chunks, int64_t per_chunk, 
     }
 }
 
-// A few rows (at most R): out (n x nn) = A B, or act(A B) * (A B2) with B2.  Bound: the weights, read once.  A
-// thread takes 16 bytes of columns and every 64th reduction element; a block 4 x 16 bytes of
-// columns, so that even a narrow layer is spread over many blocks.
-constexpr int kFewCols = 4, kFewLanes = kFfnThreads / kFewCols;
+// A few rows (at most R): out (n x nn) = A B, or act(A B) * (A B2) with B2.  Bound: the latency of one round of loads and of
+// the sum over a block.  A thread takes 16 bytes of columns of every (threads / 4)-th reduction element, a block 4 x 16 bytes
+// of columns, so that even a narrow layer is spread over many blocks and a thread has few elements.  The lanes' sums are
+// added by halves (each lane passes on half of its values, then a quarter, ...): a quarter of the exchanges of adding every
+// value over all lanes.
+constexpr int kFewCols = 4;
+
+template <int R>
+constexpr int few_threads() { return R < 4 ? 1024 : 512; }   // (the registers of four rows' sums allow no more)
+
+// v[0 .. N) summed over the lanes that differ in the bits of DIST, DIST / 2, ..., kFewCols; on return each lane holds the sums
+// of N / (their number) values (at least one) in v[0 ..], from value `first` on.
+template <int N, int DIST>
+__device__ __forceinline__ void few_reduce(float* v, int& first) {
+    if constexpr (DIST >= kFewCols) {
+        const bool up = threadIdx.x & DIST;
+        if constexpr (N > 1) {
+#pragma unroll
+            for (int i = 0; i < N / 2; ++i) {
+                const float send = up ? v[i] : v[i + N / 2], keep = up ? v[i + N / 2] : v[i];
+                v[i] = keep + __shfl_xor(send, DIST, 64);
+            }
+            first += up ? N / 2 : 0;
+            few_reduce<N / 2, DIST / 2>(v, first);
+        } else {
+            v[0] += __shfl_xor(v[0], DIST, 64);
+            few_reduce<1, DIST / 2>(v, first);
+        }
+    }
+}
 
 template <typename TA, typename T, typename TO, int R, bool GATED>
-__global__ void __launch_bounds__(kFfnThreads)
+__global__ void __launch_bounds__(few_threads<R>())
 k_ffn_few(const TA* __restrict__ A, int64_t lda, int n, int k, const T* __restrict__ B, const T* __restrict__ B2, int nn,
           int act, TO* __restrict__ out, int64_t ldo) {
     typedef RowVec<T> RV;
-    constexpr int V = RV::V, NB = GATED ? 2 : 1;
-    __shared__ float red[kFfnThreads / 64][NB * R * V * kFewCols];
+    constexpr int V = RV::V, NB = GATED ? 2 : 1, N = NB * R * V, THREADS = few_threads<R>(), LANES = THREADS / kFewCols;
+    constexpr int KEEP = N > 16 ? N / 16 : 1;   // values of a lane after the sum over its wave's 16 reduction lanes
+    __shared__ float red[THREADS / 64][N * kFewCols];
     const int cl = threadIdx.x % kFewCols, kl = threadIdx.x / kFewCols;
     const int col = (blockIdx.x * kFewCols + cl) * V;
-    float acc[NB][R][V];
+    float acc[N];
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int e = 0; e < V; ++e) acc[b][r][e] = 0.f;
+    for (int i = 0; i < N; ++i) acc[i] = 0.f;
 #pragma unroll 4
-    for (int j = kl; j < k; j += kFewLanes) {
+    for (int j = kl; j < k; j += LANES) {
         typename RV::Raw w[NB];
         w[0] = load_vec<T, true>(B + (int64_t)j * nn + col, nn - col);
         if (GATED) w[NB - 1] = load_vec<T, true>(B2 + (int64_t)j * nn + col, nn - col);
@@ -528,29 +551,23 @@ k_ffn_few(const TA* __restrict__ A, int64_t lda, int n, int k, const T* __restri
 #pragma unroll
             for (int b = 0; b < NB; ++b)
 #pragma unroll
-                for (int e = 0; e < V; ++e) acc[b][r][e] = fmaf(a, RV::get(w[b], e), acc[b][r][e]);
+                for (int e = 0; e < V; ++e) acc[(b * R + r) * V + e] = fmaf(a, RV::get(w[b], e), acc[(b * R + r) * V + e]);
         }
     }
-    const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+    int first = 0;
+    few_reduce<N, 32>(acc, first);
+    const int wave = threadIdx.x >> 6;
+    // (with fewer values than lanes several lanes hold the same sum)
 #pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int r = 0; r < R; ++r)
-#pragma unroll
-            for (int e = 0; e < V; ++e) {
-                float s = acc[b][r][e];
-#pragma unroll
-                for (int d = kFewCols; d < 64; d <<= 1) s += __shfl_xor(s, d, 64);
-                if (lane < kFewCols) red[wave][((b * R + r) * kFewCols + cl) * V + e] = s;
-            }
+    for (int i = 0; i < KEEP; ++i) red[wave][(first + i) * kFewCols + cl] = acc[i];
     __syncthreads();
-    for (int i = threadIdx.x; i < R * kFewCols * V; i += kFfnThreads) {
-        const int r = i / (kFewCols * V), c = blockIdx.x * kFewCols * V + i % (kFewCols * V);
+    for (int i = threadIdx.x; i < R * kFewCols * V; i += THREADS) {
+        const int r = i / (kFewCols * V), c4 = i / V % kFewCols, e = i % V, c = (blockIdx.x * kFewCols + c4) * V + e;
         float v[NB];
 #pragma unroll
         for (int b = 0; b < NB; ++b) {
             v[b] = 0.f;
-            for (int w = 0; w < kFfnThreads / 64; ++w) v[b] += red[w][b * R * kFewCols * V + i];
+            for (int w = 0; w < THREADS / 64; ++w) v[b] += red[w][((b * R + r) * V + e) * kFewCols + c4];
         }
         if (r >= n || c >= nn) continue;
         float o = v[0];
@@ -794,9 +811,10 @@ static void ffn_fwd_few(const FfnShape& d, const FfnLayout& L, const T* X, const
     auto* up = n == 1 ? k_ffn_few<T, T, float, 1, true> : (n == 2 ? k_ffn_few<T, T, float, 2, true> : k_ffn_few<T, T, float, 4, true>);
     auto* down = n == 1 ? k_ffn_few<float, T, T, 1, false>
                         : (n == 2 ? k_ffn_few<float, T, T, 2, false> : k_ffn_few<float, T, T, 4, false>);
-    hipLaunchKernelGGL(up, dim3((unsigned)ceil_div(d.f, W)), dim3(kFfnThreads), 0, s, X, (int64_t)d.ci, n, d.ci, Wg, Wu,
-                       d.f, act, H, d.fp);
-    hipLaunchKernelGGL(down, dim3((unsigned)ceil_div(d.co, W)), dim3(kFfnThreads), 0, s, (const float*)H, d.fp, n, d.f, Wd,
+    const int threads = n <= 2 ? few_threads<1>() : few_threads<4>();
+    hipLaunchKernelGGL(up, dim3((unsigned)ceil_div(d.f, W)), dim3(threads), 0, s, X, (int64_t)d.ci, n, d.ci, Wg, Wu, d.f, act,
+                       H, d.fp);
+    hipLaunchKernelGGL(down, dim3((unsigned)ceil_div(d.co, W)), dim3(threads), 0, s, (const float*)H, d.fp, n, d.f, Wd,
                        (const T*)nullptr, d.co, act, Y, (int64_t)d.co);
 }
 
