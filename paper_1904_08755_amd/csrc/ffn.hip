@@ -313,13 +313,14 @@ k_ffn_gemm_bf16(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n,
     store_tile(acc, r0 + 16 * MT * (wave / WN), c0 + 64 * (wave % WN), n, co, Out, co);
 }
 
-// Out (n x co) = A1 B1 + A2 B2 for KC operands in tiles of 256 rows by 64 TN columns: eight waves of 64 x 32 TN (v_mfma_f32_32x32x16_bf16), a ring
-// of four stages of 32 reduction elements, each an array of its own: the operands are plain reads, which the compiler
-// starts ahead of the products without waiting for copies into other stages.
-template <int TN>
+// Out (n x co) = A1 B1 + A2 B2 for KC operands in tiles of 256 x 256: eight waves of 64 x 128 (v_mfma_f32_32x32x16_bf16), a
+// ring of four stages of 32 reduction elements, each an array of its own: the operands are plain reads, which the compiler
+// starts ahead of the products without waiting for copies into other stages.  Bound: about as much time in the copies as in
+// the products (300,000 rows, 256 columns, 2 x 1,024 elements: 391 us; without the copies 288, without the products 368).
 __global__ void __launch_bounds__(512, 1)
 k_ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, int64_t k, const uint16_t* __restrict__ B1,
               const uint16_t* __restrict__ B2, int64_t ldb, int co, uint16_t* __restrict__ Out, int nc) {
+    constexpr int TN = 4;   // 32-column tiles of a wave
     constexpr int BN = 64 * TN, STAGE = (256 + BN) * 64;
     typedef FbCopy<FB_KC, 256, 8, true> CA;
     typedef FbCopy<FB_KC, BN, 8, true> CB;
@@ -409,12 +410,6 @@ k_ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, i
             res_store<false>(Out, co, r0 + 64 * wm + 32 * m, n, c0 + 32 * (TN * wn + t), co, o);
         }
 }
-// (named: the host compilation leaves the second of two implicit instances out)
-template __global__ void k_ffn_gemm_kc<2>(RowMat<const uint16_t>, RowMat<const uint16_t>, int64_t, int64_t, const uint16_t*,
-                                          const uint16_t*, int64_t, int, uint16_t*, int);
-template __global__ void k_ffn_gemm_kc<4>(RowMat<const uint16_t>, RowMat<const uint16_t>, int64_t, int64_t, const uint16_t*,
-                                          const uint16_t*, int64_t, int, uint16_t*, int);
-
 // H, dG and dU of a tile of 128 rows by 64 hidden columns.
 template <int MT>
 __global__ void __launch_bounds__(256, 2)
@@ -609,10 +604,23 @@ struct FfnLayout {
     int tn0, t0, tn1, t1;
 };
 
-// Rows from which the kernels that keep rows in registers take them (bfloat16).
-constexpr int64_t kResFwdRows = 128 * 256, kResBwdRows = 128 * 64;
-static bool ffn_resident(const FfnShape& d, bool bwd) {
-    return d.ci <= kResMax && d.co <= kResMax && d.n >= (bwd ? kResBwdRows : kResFwdRows);
+// Whether the kernels that keep rows in registers can take a bfloat16 call at all.
+static bool ffn_res_can(const FfnShape& d) { return d.ci <= kResMax && d.co <= kResMax; }
+
+// ... and do.  Forward, up to 128 channels: from about 100 tiles of 128 rows on (16,000 rows of 128 channels 20 us, tiles 21; of
+// 100 channels, which tiles have to copy first, 14 and 21; 8,000 rows of 128 channels 19 and 16).  Wider ones take a block a
+// compute unit: where the last round of blocks leaves less than a quarter of the device idle (256 channels: 30,000 rows 55
+// and 61 us, 45,000 rows in a second round of 96 blocks 96 and 84, 60,000 rows 102 and 112).
+static bool ffn_res_fwd(const FfnShape& d) {
+    const int64_t tiles = ceil_div(d.n, 128), cus = device_cus();
+    if (!ffn_res_can(d)) return false;
+    return d.ci <= 128 && d.co <= 128 ? tiles >= 100 : 4 * tiles >= 3 * ceil_div(tiles, cus) * cus;
+}
+// Backward: once H, dG and dU outgrow the 256 MB of the last-level cache, where the tiles' traffic costs more than their better
+// spread over the device saves (forward and backward of 128 channels, 512 hidden: 60,000 rows 155 us, tiles 148; 90,000 rows
+// 217 and 224; 200,000 rows 471 and 519), and not for 64 channels or less (200,000 rows of 64: 221 and 215).
+static bool ffn_res_bwd(const FfnShape& d) {
+    return ffn_res_can(d) && (d.ci > 64 || d.co > 64) && d.n * d.fp * 6 >= (int64_t)256 << 20;
 }
 
 // float32: tiles of 64 outputs instead of 128 in a direction where they leave less of the last one empty.
@@ -644,7 +652,7 @@ static FfnLayout ffn_layout(int dtype, const FfnShape& d, bool bwd) {
         L.wg = take((size_t)d.ci * pad8(d.f) * 2);
         L.wu = take((size_t)d.ci * pad8(d.f) * 2);
         L.wd = take((size_t)d.f * pad8(d.co) * 2);
-        if (ffn_resident(d, bwd)) L.pack = take(res_pack_bytes(d.ci, d.f, d.co, bwd));
+        if (ffn_res_can(d)) L.pack = take(res_pack_bytes(d.ci, d.f, d.co));
     }
     const int64_t tiles = ceil_div(d.n, 128);
     L.h = take((size_t)(!bwd && d.n <= kFfnFewRows ? d.n * 4 : tiles * 128 * size) * d.fp);
@@ -762,7 +770,7 @@ static void ffn_gemm_bf16(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, 
 static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const uint16_t* X, const uint16_t* Wg, const uint16_t* Wu,
                     const uint16_t* Wd, int act, uint16_t* Y, char* ws, hipStream_t s) {
     const RowMat<uint16_t> H = row_blocks(reinterpret_cast<uint16_t*>(ws + L.h), d.fp);
-    if (ffn_resident(d, false)) {
+    if (ffn_res_fwd(d)) {
         res_fwd(X, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, Y, ws + L.pack, s);
         return;
     }
@@ -786,18 +794,14 @@ static void ffn_dw(const FfnLayout& L, const DwSide<uint16_t>& p0, const DwSide<
                        L.per_chunk, part);
 }
 
-constexpr int64_t kGemmKcRows = 128 * 256;
-static void ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, int64_t k, const uint16_t* B1,
-                        const uint16_t* B2, int64_t ldb, int co, uint16_t* Out, hipStream_t s) {
-    if (co <= 64 || n < kGemmKcRows) return ffn_gemm_bf16<FB_KC>(A1, A2, n, k, B1, B2, ldb, co, Out, s);
-    auto launch = [&](auto TN) {
-        constexpr int tn = decltype(TN)::value;
-        const int nc = (int)ceil_div(co, 64 * tn);
-        hipLaunchKernelGGL(k_ffn_gemm_kc<tn>, dim3((unsigned)(ceil_div(n, 256) * nc)), dim3(512), 0, s, A1, A2, n, k, B1, B2, ldb, co,
-                           Out, nc);
-    };
-    if (co > 128) launch(std::integral_constant<int, 4>{});
-    else launch(std::integral_constant<int, 2>{});
+// Tiles of 256 x 256 where they fill the device and are not mostly empty (60,000 rows of 256 channels, 1,024 hidden: 27 us of
+// the whole backward pass; no difference at 128 channels).
+static void ffn_dx_bf16(RowMat<const uint16_t> dG, RowMat<const uint16_t> dU, int64_t n, int64_t f, const uint16_t* Wg,
+                        const uint16_t* Wu, int64_t ldw, int ci, uint16_t* dX, hipStream_t s) {
+    if (ci <= 128 || n < 256 * 128) return ffn_gemm_bf16<FB_KC>(dG, dU, n, f, Wg, Wu, ldw, ci, dX, s);
+    const int nc = (int)ceil_div(ci, 256);
+    hipLaunchKernelGGL(k_ffn_gemm_kc, dim3((unsigned)(ceil_div(n, 256) * nc)), dim3(512), 0, s, dG, dU, n, f, Wg, Wu, ldw, ci,
+                       dX, nc);
 }
 
 // --- either type
@@ -840,13 +844,13 @@ static void ffn_bwd(const FfnShape& d, const FfnLayout& L, const T* X, const T* 
             ldx = x.ld;
             ldy = y.ld;
             const int nf = (int)ceil_div(d.f, 64);
-            if (ffn_resident(d, true)) {
+            if (ffn_res_bwd(d)) {
                 res_mid(X, dY, n, d.ci, Wg, Wu, d.f, Wd, d.co, act, H, dG, dU, ws + L.pack, s);
             } else {
                 hipLaunchKernelGGL(k_ffn_mid_bf16<4>, dim3((unsigned)(ceil_div(n, 128) * nf)), dim3(256), 0, s, x.p, x.ld,
                                    y.p, y.ld, n, d.ci, d.co, g.p, u.p, g.ld, w.p, w.ld, d.f, act, H, dG, dU, nf);
             }
-            if (dX) ffn_gemm_kc(ffn_const(dG), ffn_const(dU), n, d.f, g.p, u.p, g.ld, d.ci, dX, s);
+            if (dX) ffn_dx_bf16(ffn_const(dG), ffn_const(dU), n, d.f, g.p, u.p, g.ld, d.ci, dX, s);
         } else {
             ffn_bwd_rows(d, X, Wg, Wu, Wd, dY, act, dX, H, dG, dU, s);
         }

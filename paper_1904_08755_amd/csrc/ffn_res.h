@@ -7,14 +7,14 @@ namespace gsc {
 
 constexpr int kResMax = 256;    // channels
 
-// Bytes of the packed weights of the forward (backward) pass.
-size_t res_pack_bytes(int ci, int f, int co, bool bwd);
+// Bytes of the packed weights of either pass.
+size_t res_pack_bytes(int ci, int f, int co);
 
 // Y (n x co) = (act(X Wg) * (X Wu)) Wd, all rows at any address; pack: res_pack_bytes of device memory, 16-byte aligned.
 void res_fwd(const uint16_t* X, int64_t n, int ci, const uint16_t* Wg, const uint16_t* Wu, int f, const uint16_t* Wd, int co,
              int act, uint16_t* Y, void* pack, hipStream_t s);
 
-// H, dG and dU (row_blocks; columns behind f up to whole 64s zero).
+// H, dG and dU (row_blocks; columns behind f up to whole 64s zero); more than 64 channels on either side.
 void res_mid(const uint16_t* X, const uint16_t* dY, int64_t n, int ci, const uint16_t* Wg, const uint16_t* Wu, int f,
              const uint16_t* Wd, int co, int act, RowMat<uint16_t> H, RowMat<uint16_t> dG, RowMat<uint16_t> dU, void* pack,
              hipStream_t s);

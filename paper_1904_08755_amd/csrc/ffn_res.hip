@@ -164,7 +164,7 @@ struct ResPairFrag {
 };
 
 // H, dG and dU of 128 rows and `per` hidden chunks from blockIdx.y * per on.  KT: 16-element steps of the
-// wider of ci and co (4, 8 or 16); W: the weights packed for it.  The block's dY lies in LDS as fragments (the registers
+// wider of ci and co (8 or 16); W: the weights packed for it.  The block's dY lies in LDS as fragments (the registers
 // hold X, a chunk's sums and those of the chunk before).
 template <int KT, int ACT>
 __global__ void __launch_bounds__(kResThreads, 1)
@@ -365,7 +365,7 @@ static int res_steps(int ci, int co) {
     return c <= 64 ? 4 : (c <= 128 ? 8 : 16);
 }
 
-size_t res_pack_bytes(int ci, int f, int co, bool) {
+size_t res_pack_bytes(int ci, int f, int co) {
     const int kt = res_steps(ci, co);
     return (size_t)((f + 63) / 64) * (res_pair_bytes(kt) + res_last_bytes(kt));
 }
@@ -374,14 +374,14 @@ static int res_pack(int ci, int f, int co, const uint16_t* Wg, const uint16_t* W
                     hipStream_t s) {
     const int kt = res_steps(ci, co);
     const ResPack p{Wg, Wu, Wd, ci, f, co, kt, back};
-    const size_t blocks = (res_pack_bytes(ci, f, co, back) + 4095) / 4096;
+    const size_t blocks = (res_pack_bytes(ci, f, co) + 4095) / 4096;
     hipLaunchKernelGGL(k_ffn_pack, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(256), 0, s, p,
                        reinterpret_cast<uint16_t*>(pack));
     return kt;
 }
 
-// f(KT, activation as constants)
-template <typename F>
+// f(KT (at least LEAST), activation as constants)
+template <int LEAST, typename F>
 static void res_with(int kt, int act, F f) {
     auto with = [&](auto KT) {
         switch (act) {
@@ -392,14 +392,15 @@ static void res_with(int kt, int act, F f) {
             default: return f(KT, std::integral_constant<int, GSC_GATE_SILU>{});
         }
     };
-    if (kt == 4) with(std::integral_constant<int, 4>{});
-    else if (kt == 8) with(std::integral_constant<int, 8>{});
+    if constexpr (LEAST <= 4)
+        if (kt == 4) return with(std::integral_constant<int, 4>{});
+    if (kt == 8) with(std::integral_constant<int, 8>{});
     else with(std::integral_constant<int, 16>{});
 }
 
 void res_fwd(const uint16_t* X, int64_t n, int ci, const uint16_t* Wg, const uint16_t* Wu, int f, const uint16_t* Wd, int co,
              int act, uint16_t* Y, void* pack, hipStream_t s) {
-    res_with(res_pack(ci, f, co, Wg, Wu, Wd, 0, pack, s), act, [&](auto KT, auto ACT) {
+    res_with<4>(res_pack(ci, f, co, Wg, Wu, Wd, 0, pack, s), act, [&](auto KT, auto ACT) {
         auto* kern = k_ffn_fwd_res<decltype(KT)::value, decltype(ACT)::value>;
         hipLaunchKernelGGL(kern, dim3((unsigned)((n + kResRows - 1) / kResRows)), dim3(kResThreads), 0, s, X, n, ci, co,
                            reinterpret_cast<const uint8_t*>(pack), f, Y);
@@ -413,7 +414,7 @@ void res_mid(const uint16_t* X, const uint16_t* dY, int64_t n, int ci, const uin
     const int64_t tiles = (n + kResRows - 1) / kResRows, chunks = (f + 63) / 64;
     const int64_t parts = tiles >= 512 ? 1 : (512 + tiles - 1) / tiles;
     const int per = (int)((chunks + parts - 1) / parts);
-    res_with(res_pack(ci, f, co, Wg, Wu, Wd, 1, pack, s), act, [&](auto KT, auto ACT) {
+    res_with<8>(res_pack(ci, f, co, Wg, Wu, Wd, 1, pack, s), act, [&](auto KT, auto ACT) {
         auto* kern = k_ffn_mid_res<decltype(KT)::value, decltype(ACT)::value>;
         hipLaunchKernelGGL(kern, dim3((unsigned)tiles, (unsigned)((chunks + per - 1) / per)), dim3(kResThreads), 0, s, X, dY, n,
                            ci, co, reinterpret_cast<const uint8_t*>(pack), f, H, dG, dU, per);

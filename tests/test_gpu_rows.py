@@ -411,6 +411,24 @@ def test_gated_ffn_many_rows(dtype, i):
     assert all(torch.equal(p, q) for p, q in zip(gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, act), grads))
 
 
+# hidden rows that outgrow the last-level cache (the backward pass in registers), and row counts on both sides of the
+# forward pass's choice: 12,672 and 12,801 rows, tiles that fill two rounds of blocks and that barely begin one
+FFN_CHOICES = [(90001, 128, 512, 96, 0), (45000, 200, 1000, 256, 1), (350003, 70, 100, 66, 0), (350001, 36, 120, 97, 1),
+               (12672, 128, 256, 64, 0), (12801, 128, 256, 64, 0), (65500, 150, 128, 130, 0), (33100, 150, 128, 130, 0)]
+
+
+@pytest.mark.parametrize("i", range(len(FFN_CHOICES)))
+def test_gated_ffn_choices(i):
+    n, ci, f, co, at = FFN_CHOICES[i]
+    act = ACTS[i % len(ACTS)]
+    X, Wg, Wu, Wd, dY = _ffn_inputs(torch.bfloat16, n, ci, f, co, at)
+    Y = gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd, act)
+    grads = gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, act)
+    _ffn_check(X, Wg, Wu, Wd, dY, act, Y, grads)
+    assert torch.equal(gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd, act), Y)
+    assert all(torch.equal(p, q) for p, q in zip(gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, act), grads))
+
+
 @BOTH
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("n", [2, 200])
