@@ -11,6 +11,8 @@
 // in the registers of LPR lanes (NV pieces of 16 bytes a lane), so it is read once; a wave holds
 // 64 / LPR rows, reduces each with log2(LPR) lane exchanges and needs no LDS, and the lanes keep
 // their columns' gamma, beta and (backward) column sums in registers over all rows they visit.
+// Measured: 300,000 rows of 256 bfloat16 columns forward 55 us (5.6 TB/s), backward 92 us and 5 us for the sums (5.0 TB/s);
+// 20,011 rows of 1,027 (rows at odd addresses, a third of the lanes idle in the last piece) 20 and 36 us (4.2 and 3.5 TB/s).
 // Rows of more than kLnRegCols columns take a block each and are read again for each sum (from the L2).
 #include "row_vec.h"
 
@@ -21,6 +23,10 @@ constexpr int kLnRegCols = 2048;       // 32 elements a lane of a wave
 constexpr int kLnMaxCols = 1 << 30;
 constexpr int64_t kLnFwdBlocks = 2048;  // blocks that walk over the rows (8 a CU)
 constexpr int64_t kLnChunks = 1024;     // row chunks (blocks) of the backward pass: as many partial column sums
+// Wide rows with many elements a lane take half as many of either: fewer blocks fit a CU, and the columns' arrays and sums that
+// a block starts and ends with are long (bfloat16 backward, 20,000 rows of 1,024 columns 27 us, 29 with all of them; 205,400
+// rows of 100 columns 70 and 45; float32, 79,922 rows of 257 columns in 12 elements a lane 51 and 44).
+static int64_t ln_most(int c, int per_lane, int64_t most) { return c > 256 && per_lane >= 16 ? most / 2 : most; }
 constexpr int kLnSumCh = 16, kLnSumLanes = 64;
 
 static int64_t ln_row_blocks(int64_t n, int rows, int64_t most) {
@@ -35,11 +41,71 @@ __device__ __forceinline__ float row_sum(float v) {
     return v;
 }
 
-// V values of a per-column float32 array (null: the value `none`), 0 behind its end
+// V values of a per-column float32 array (null: the value `none`), 0 behind its end: 16-byte loads, which a wave
+// pays for once over all of its rows (element by element they took longer than a row did).
 template <int V>
 __device__ __forceinline__ void load_cols(const float* p, int col, int c, float none, float (&v)[V]) {
 #pragma unroll
-    for (int e = 0; e < V; ++e) v[e] = col + e < c ? (p ? p[col + e] : none) : 0.f;
+    for (int h = 0; h < V; h += 4) {
+        RowVec<float>::Raw r = {0, 0, 0, 0};
+        if (p) r = load_vec<float, true>(p + col + h, c - col - h);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[h + e] = p ? __uint_as_float(r[e]) : (col + h + e < c ? none : 0.f);
+    }
+}
+
+// Whether piece i of every lane is a whole one (the shapes of ln_dispatch but the widest need all their pieces).
+template <int NV>
+constexpr bool ln_whole(int i) { return i < NV - 1 && NV <= 4; }
+
+// A row's pieces of one lane: piece i holds the V elements from column (i LPR + l) V on, zeros behind the end.  A partial
+// piece is the row's last 16 bytes, shifted (loads of its elements one by one took as long as the rest of the row).
+template <typename T, int LPR, int NV, bool TAIL>
+__device__ __forceinline__ void load_row(const T* x, int l, int c, typename RowVec<T>::Raw (&raw)[NV]) {
+    constexpr int V = RowVec<T>::V;
+    typedef typename RowVec<T>::Raw Raw;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+        const int col = (i * LPR + l) * V;
+        if (ln_whole<NV>(i)) raw[i] = *reinterpret_cast<const Raw*>(x + col);
+        else if (!TAIL || c < V) raw[i] = load_vec<T, TAIL>(x + col, c - col);
+        else {
+            Raw r = {0, 0, 0, 0};
+            if (col < c) r = *reinterpret_cast<const Raw*>(x + (col + V <= c ? col : c - V));
+            if (col + V > c) {
+                const int sh = (V - c % V) * 8 * (int)sizeof(T);   // 16 .. 112 bits, the same for all lanes
+                const uint64_t lo = (uint64_t)r[1] << 32 | r[0], hi = (uint64_t)r[3] << 32 | r[2];
+                const uint64_t a = sh >= 64 ? hi >> (sh - 64) : lo >> sh | hi << (64 - sh), b = sh >= 64 ? 0 : hi >> sh;
+                r = Raw{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+            }
+            raw[i] = r;
+        }
+    }
+}
+// ... and back: the partial piece in stores of 8, 4 and 2 bytes.
+template <typename T, int NV, bool TAIL>
+__device__ __forceinline__ void store_piece(T* y, int i, int col, int c, const float (&v)[RowVec<T>::V]) {
+    typedef RowVec<T> R;
+    typedef typename R::Raw Raw;
+    if (ln_whole<NV>(i) || col + R::V <= c) {
+        *reinterpret_cast<Raw*>(y + col) = R::put(v);
+    } else if (TAIL && col < c) {
+        const Raw r = R::put(v);
+        uint32_t* p = reinterpret_cast<uint32_t*>(y + col);   // (at any element's address)
+        const int bytes = (c % R::V) * (int)sizeof(T);
+        if (bytes & 8) {
+            typedef uint32_t Two __attribute__((ext_vector_type(2), aligned(2)));
+            *reinterpret_cast<Two*>(p) = Two{r[0], r[1]};
+        }
+        if (bytes & 4) {
+            typedef uint32_t One __attribute__((aligned(2)));
+            *reinterpret_cast<One*>(p + (bytes >> 3) * 2) = bytes & 8 ? r[2] : r[0];
+        }
+        if (sizeof(T) == 2 && (bytes & 2)) {
+            const uint32_t w = bytes & 8 ? (bytes & 4 ? r[3] : r[2]) : (bytes & 4 ? r[1] : r[0]);
+            *reinterpret_cast<uint16_t*>(p + (bytes >> 2)) = (uint16_t)w;
+        }
+    }
 }
 
 template <typename T, int LPR, int NV, bool TAIL>
@@ -57,20 +123,15 @@ __global__ void __launch_bounds__(kLnThreads) k_ln_fwd(const T* X, int64_t n, in
         load_cols<V>(beta, (i * LPR + l) * V, c, 0.f, be[i]);
     }
     for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR; row < n; row += (int64_t)gridDim.x * RPB) {
-        const T* x = X + row * c;
         typename R::Raw raw[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int col = (i * LPR + l) * V;
-            raw[i] = load_vec<T, TAIL>(x + col, c - col);
-        }
+        load_row<T, LPR, NV, TAIL>(X + row * c, l, c, raw);
         const float x0 = __shfl(R::get(raw[0], 0), 0, LPR);   // the row's first element
         float v[NV][V], s = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const bool in = (i * LPR + l) * V + (TAIL ? e : 0) < c;
+                const bool in = ln_whole<NV>(i) || (i * LPR + l) * V + (TAIL ? e : 0) < c;
                 v[i][e] = in ? R::get(raw[i], e) - x0 : 0.f;
                 s += v[i][e];
             }
@@ -80,7 +141,7 @@ __global__ void __launch_bounds__(kLnThreads) k_ln_fwd(const T* X, int64_t n, in
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const bool in = (i * LPR + l) * V + (TAIL ? e : 0) < c;
+                const bool in = ln_whole<NV>(i) || (i * LPR + l) * V + (TAIL ? e : 0) < c;
                 v[i][e] = in ? v[i][e] - m : 0.f;
                 q = fmaf(v[i][e], v[i][e], q);
             }
@@ -91,7 +152,7 @@ __global__ void __launch_bounds__(kLnThreads) k_ln_fwd(const T* X, int64_t n, in
             float o[V];
 #pragma unroll
             for (int e = 0; e < V; ++e) o[e] = fmaf(v[i][e] * r, ga[i][e], be[i][e]);
-            store_vec<T, TAIL>(Y + row * c + col, c - col, o);
+            store_piece<T, NV, TAIL>(Y + row * c, i, col, c, o);
         }
         if (l == 0) {
             if (mean) mean[row] = x0 + m;
@@ -157,22 +218,16 @@ __global__ void __launch_bounds__(kLnThreads) k_ln_bwd(const T* X, const T* dY, 
         for (int e = 0; e < V; ++e) sg[i][e] = sb[i][e] = 0.f;
     }
     for (int64_t row = (int64_t)blockIdx.x * RPB + threadIdx.x / LPR; row < n; row += (int64_t)gridDim.x * RPB) {
-        const T* x = X + row * c;
-        const T* dy = dY + row * c;
         typename R::Raw xr[NV], yr[NV];
-#pragma unroll
-        for (int i = 0; i < NV; ++i) {
-            const int col = (i * LPR + l) * V;
-            xr[i] = load_vec<T, TAIL>(x + col, c - col);
-            yr[i] = load_vec<T, TAIL>(dy + col, c - col);
-        }
+        load_row<T, LPR, NV, TAIL>(X + row * c, l, c, xr);
+        load_row<T, LPR, NV, TAIL>(dY + row * c, l, c, yr);
         const float m = mean[row], r = rstd[row];
         float a = 0.f, b = 0.f;   // sums of g and of g h
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
-                const bool in = (i * LPR + l) * V + (TAIL ? e : 0) < c;
+                const bool in = ln_whole<NV>(i) || (i * LPR + l) * V + (TAIL ? e : 0) < c;
                 const float h = in ? (R::get(xr[i], e) - m) * r : 0.f;
                 const float d = R::get(yr[i], e), g = d * ga[i][e];
                 sg[i][e] = fmaf(d, h, sg[i][e]);
@@ -192,7 +247,7 @@ __global__ void __launch_bounds__(kLnThreads) k_ln_bwd(const T* X, const T* dY, 
                     const float h = (R::get(xr[i], e) - m) * r;
                     o[e] = r * (R::get(yr[i], e) * ga[i][e] - a - h * b);
                 }
-                store_vec<T, TAIL>(dX + row * c + col, c - col, o);
+                store_piece<T, NV, TAIL>(dX + row * c, i, col, c, o);
             }
         }
     }
@@ -293,38 +348,38 @@ k_ln_bwd_sum(const float* __restrict__ part, int64_t chunks, int c, float* __res
     }
 }
 
-// f(LPR, NV, TAIL as constants) for rows of c <= kLnRegCols columns: the fewest lanes a row that hold
-// it in `most` pieces a lane, a whole wave with more pieces for the widest.
+// f(LPR, NV, TAIL as constants) for rows of c <= kLnRegCols columns: of the shapes of at most MOST pieces a lane the one
+// that holds the row with the fewest pieces in all, with more lanes a row among equals; a whole wave
+// with more pieces for the widest rows.
 template <typename T, int MOST, typename F>
 static void ln_dispatch(int c, F f) {
     constexpr int V = RowVec<T>::V;
     const int vecs = (c + V - 1) / V;
     const bool tail = c % V != 0;
+    int lpr = 64, nv = (vecs + 63) / 64;
+    for (int l = 32; l >= 8; l /= 2) {
+        const int k = (vecs + l - 1) / l;
+        if (k <= MOST && l * k < lpr * nv) lpr = l, nv = k;
+    }
     auto with = [&](auto LPR, auto NV) {
         if (tail) f(LPR, NV, std::true_type{});
         else f(LPR, NV, std::false_type{});
     };
-    auto lanes = [&](auto LPR) {
-        constexpr int L = decltype(LPR)::value;
-        const int nv = (vecs + L - 1) / L;
-        if (nv <= 1) return with(LPR, std::integral_constant<int, 1>{});
-        if (MOST == 2 || nv == 2) return with(LPR, std::integral_constant<int, 2>{});
-        if constexpr (MOST > 2) {
-            if (nv == 3) return with(LPR, std::integral_constant<int, 3>{});
-            return with(LPR, std::integral_constant<int, 4>{});
+    auto pieces = [&](auto LPR) {
+        if (nv == 1) return with(LPR, std::integral_constant<int, 1>{});
+        if (nv == 2) return with(LPR, std::integral_constant<int, 2>{});
+        if (nv == 3) return with(LPR, std::integral_constant<int, 3>{});
+        if constexpr (MOST > 3 || decltype(LPR)::value == 64)
+            if (nv == 4) return with(LPR, std::integral_constant<int, 4>{});
+        if constexpr (V == 4 && decltype(LPR)::value == 64) {   // float32 rows: up to 512 pieces
+            if (nv <= 6) return with(LPR, std::integral_constant<int, 6>{});
+            return with(LPR, std::integral_constant<int, 8>{});
         }
     };
-    if (vecs <= 8 * MOST) return lanes(std::integral_constant<int, 8>{});
-    if (vecs <= 16 * MOST) return lanes(std::integral_constant<int, 16>{});
-    if (vecs <= 32 * MOST) return lanes(std::integral_constant<int, 32>{});
-    if (vecs <= 64 * MOST) return lanes(std::integral_constant<int, 64>{});
-    constexpr std::integral_constant<int, 64> W{};
-    if (MOST == 2 && vecs <= 64 * 3) return with(W, std::integral_constant<int, 3>{});
-    if (MOST == 2 && vecs <= 64 * 4) return with(W, std::integral_constant<int, 4>{});
-    if constexpr (V == 4) {   // float32 rows: up to 512 pieces
-        if (vecs <= 64 * 6) return with(W, std::integral_constant<int, 6>{});
-        return with(W, std::integral_constant<int, 8>{});
-    }
+    if (lpr == 64) pieces(std::integral_constant<int, 64>{});
+    else if (lpr == 32) pieces(std::integral_constant<int, 32>{});
+    else if (lpr == 16) pieces(std::integral_constant<int, 16>{});
+    else pieces(std::integral_constant<int, 8>{});
 }
 
 template <typename T>
@@ -337,10 +392,10 @@ static void ln_fwd(const void* X_, int64_t n, int c, const float* gamma, const f
                            X, n, c, gamma, beta, eps, Y, mean, rstd);
         return;
     }
-    ln_dispatch<T, 4>(c, [&](auto LPR, auto NV, auto TAIL) {
+    ln_dispatch<T, 3>(c, [&](auto LPR, auto NV, auto TAIL) {
         constexpr int L = decltype(LPR)::value, N = decltype(NV)::value;
         auto* kern = k_ln_fwd<T, L, N, decltype(TAIL)::value>;
-        hipLaunchKernelGGL(kern, dim3((unsigned)ln_row_blocks(n, kLnThreads / L, kLnFwdBlocks)), dim3(kLnThreads), 0, s,
+        hipLaunchKernelGGL(kern, dim3((unsigned)ln_row_blocks(n, kLnThreads / L, ln_most(c, N * RowVec<T>::V, kLnFwdBlocks))), dim3(kLnThreads), 0, s,
                            X, n, c, gamma, beta, eps, Y, mean, rstd);
     });
 }
@@ -364,10 +419,10 @@ static int64_t ln_bwd(const void* X_, const void* dY_, int64_t n, int c, const f
                                0, s, X, dY, n, c, gamma, mean, rstd, dX);
         return chunks;
     }
-    ln_dispatch<T, 2>(c, [&](auto LPR, auto NV, auto TAIL) {
+    ln_dispatch<T, 3>(c, [&](auto LPR, auto NV, auto TAIL) {
         constexpr int L = decltype(LPR)::value, N = decltype(NV)::value;
         auto* kern = k_ln_bwd<T, L, N, decltype(TAIL)::value>;
-        chunks = ln_row_blocks(n, kLnThreads / L, kLnChunks);
+        chunks = ln_row_blocks(n, kLnThreads / L, ln_most(c, N * RowVec<T>::V, kLnChunks));
         hipLaunchKernelGGL(kern, dim3((unsigned)chunks), dim3(kLnThreads),
                            part ? (kLnThreads / 64) * c * sizeof(float) : 0, s, X, dY, n, c, gamma, mean, rstd, dX,
                            part);
