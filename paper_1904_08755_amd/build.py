@@ -21,7 +21,7 @@ BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libgsc.so")
 SOURCES = ["common.hip", "coords.hip", "kmap.hip", "plan.hip", "conv.hip", "conv_bf16.hip", "conv_blk.hip",
            "conv_tile.hip", "pool.hip", "norm.hip", "rotary.hip", "ffn.hip",
-           "ffn_res.hip"]
+           "ffn_res.hip", "ffn_res_f32.hip"]
 ARCH = "gfx950"
 
 COMMON_FLAGS = [

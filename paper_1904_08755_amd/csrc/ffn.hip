@@ -623,6 +623,8 @@ static bool ffn_res_bwd(const FfnShape& d) {
     return ffn_res_can(d) && (d.ci > 64 || d.co > 64) && d.n * d.fp * 6 >= (int64_t)256 << 20;
 }
 
+static bool ffn_res_f32(const FfnShape& d) { return d.ci <= kResMaxF32 && d.co <= kResMaxF32 && d.n >= 8192; }
+
 // float32: tiles of 64 outputs instead of 128 in a direction where they leave less of the last one empty.
 static bool ffn_narrow(int64_t rows) { return ceil_div(rows, 64) % 2 == 1 && rows < 512; }
 
@@ -706,6 +708,7 @@ static void ffn_gemm_f32(RowMat<const float> A1, RowMat<const float> A2, int64_t
 
 static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const float* X, const float* Wg, const float* Wu,
                     const float* Wd, int act, float* Y, char* ws, hipStream_t s) {
+    if (ffn_res_f32(d)) return res_fwd(X, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, Y, s);
     const RowMat<float> H = row_blocks(reinterpret_cast<float*>(ws + L.h), d.fp);
     const int nf = (int)ceil_div(d.f, 64);
     const bool sho = ffn_short(d.n, 128, nf);
@@ -718,6 +721,7 @@ static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const float* X, const
 static void ffn_bwd_rows(const FfnShape& d, const float* X, const float* Wg, const float* Wu, const float* Wd,
                          const float* dY, int act, float* dX, RowMat<float> H, RowMat<float> dG, RowMat<float> dU,
                          hipStream_t s) {
+    if (ffn_res_f32(d)) return res_bwd(X, dY, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, (int)d.fp, H, dG, dU, dX, s);
     const int nf = (int)ceil_div(d.f, 64);
     const bool sho = ffn_short(d.n, 128, nf);
     auto* mid = sho ? k_ffn_mid_f32<2> : k_ffn_mid_f32<4>;
