@@ -151,7 +151,7 @@ __device__ __forceinline__ void store_mid(const floatx4 (&acc)[MT][4], const flo
 // float32 kernels: tiles of 32 MT rows
 // ---------------------------------------------------------------------------
 // H (columns behind f zero) of a tile by 64 hidden columns.
-template <int MT>
+template <int MT, bool WHOLE>
 __global__ void __launch_bounds__(kFfnThreads, 2)
 k_ffn_up_f32(const float* __restrict__ X, int64_t n, int ci, const float* __restrict__ Wg, const float* __restrict__ Wu,
              int f, int act, RowMat<float> H, int nf) {
@@ -161,13 +161,13 @@ k_ffn_up_f32(const float* __restrict__ X, int64_t n, int ci, const float* __rest
     const int c0 = (int)(u % nf) * 64, wave = threadIdx.x >> 6;
     floatx4 acc[MT][4];
     zero_acc(acc);
-    tile_product<true, false, MT, 4, true>({row_major(X + r0 * ci, ci), nullptr, n - r0, ci},
+    tile_product<true, false, MT, 4, true, WHOLE>({row_major(X + r0 * ci, ci), nullptr, n - r0, ci},
                                            {row_major(Wg + c0, f), Wu + c0, f - c0, ci}, lds, acc);
     store_hidden(acc, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H);
 }
 
 // Out (n x co) = A1 B1 (+ A2 B2 where A2 is given) over k: A rows of the reduction (KC), B (row-major) either way.
-template <bool BKC, int MT, int NT>
+template <bool BKC, int MT, int NT, bool WHOLE>
 __global__ void __launch_bounds__(kFfnThreads, 2)
 k_ffn_gemm_f32(RowMat<const float> A1, RowMat<const float> A2, int64_t n, int64_t k, const float* __restrict__ B1,
                const float* __restrict__ B2, int64_t ldb, int co, float* __restrict__ Out, int nc) {
@@ -181,7 +181,7 @@ k_ffn_gemm_f32(RowMat<const float> A1, RowMat<const float> A2, int64_t n, int64_
         const RowMat<const float> A = s ? A2 : A1;
         const float* B = s ? B2 : B1;
         if (!A.p) break;
-        tile_product<true, BKC, MT, NT, false>({A.at(r0, 0), nullptr, n - r0, k},
+        tile_product<true, BKC, MT, NT, false, WHOLE>({A.at(r0, 0), nullptr, n - r0, k},
                                                {row_major(BKC ? B + (int64_t)c0 * ldb : B + c0, ldb), nullptr, co - c0, k},
                                                lds, acc);
     }
@@ -189,7 +189,7 @@ k_ffn_gemm_f32(RowMat<const float> A1, RowMat<const float> A2, int64_t n, int64_
 }
 
 // H, dG and dU of a tile by 64 hidden columns.
-template <int MT>
+template <int MT, bool WHOLE>
 __global__ void __launch_bounds__(kFfnThreads, 2)
 k_ffn_mid_f32(const float* __restrict__ X, const float* __restrict__ dY, int64_t n, int ci, int co,
               const float* __restrict__ Wg, const float* __restrict__ Wu, const float* __restrict__ Wd, int f, int act,
@@ -201,9 +201,9 @@ k_ffn_mid_f32(const float* __restrict__ X, const float* __restrict__ dY, int64_t
     floatx4 acc[MT][4], dh[MT][2];
     zero_acc(acc);
     zero_acc(dh);
-    tile_product<true, false, MT, 4, true>({row_major(X + r0 * ci, ci), nullptr, n - r0, ci},
+    tile_product<true, false, MT, 4, true, WHOLE>({row_major(X + r0 * ci, ci), nullptr, n - r0, ci},
                                            {row_major(Wg + c0, f), Wu + c0, f - c0, ci}, lds, acc);
-    tile_product<true, true, MT, 2, false>({row_major(dY + r0 * co, co), nullptr, n - r0, co},
+    tile_product<true, true, MT, 2, false, WHOLE>({row_major(dY + r0 * co, co), nullptr, n - r0, co},
                                            {row_major(Wd + (int64_t)c0 * co, co), nullptr, f - c0, co}, lds, dh);
     store_mid(acc, dh, r0 + 16 * MT * (wave >> 1), c0 + 32 * (wave & 1), n, act, H, dG, dU);
 }
@@ -217,25 +217,29 @@ struct DwSide {
     int64_t part;      // where its sums start in a chunk's partial sums
 };
 
-// Partial sums of both products over the rows of a chunk.
-template <int MT, int NT>
-__global__ void __launch_bounds__(kFfnThreads, 2)
-k_ffn_dw_f32(DwSide<float> p0, DwSide<float> p1, int64_t n, int64_t chunk, int64_t per_chunk, float* __restrict__ part) {
-    __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<MT, NT>()];
-    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
-    const int tiles = p0.tiles + p1.tiles;
-    const int64_t s = u / tiles;
-    int t = (int)(u - s * tiles);
-    const bool second = t >= p0.tiles;
-    const DwSide<float> p = second ? p1 : p0;
-    if (second) t -= p0.tiles;
+// Partial sums of a tile of 32 MT x 32 NT of one product over a chunk's rows
+template <int MT, int NT, bool WHOLE>
+__device__ __forceinline__ void dw_tile_f32(const DwSide<float>& p, int t, int64_t r0, int64_t rows, uint8_t* lds, float* out) {
     const int m0 = t / p.tn * (32 * MT), c0 = t % p.tn * (32 * NT), wave = threadIdx.x >> 6;
-    const int64_t r0 = s * chunk, rows = n - r0 < chunk ? n - r0 : chunk;
     floatx4 acc[MT][NT];
     zero_acc(acc);
-    tile_product<false, false, MT, NT, false>({p.A.at(r0, m0), nullptr, p.m - m0, rows},
+    tile_product<false, false, MT, NT, false, WHOLE>({p.A.at(r0, m0), nullptr, p.m - m0, rows},
                                               {p.B.at(r0, c0), nullptr, p.nn - c0, rows}, lds, acc);
-    store_tile(acc, m0 + 16 * MT * (wave >> 1), c0 + 16 * NT * (wave & 1), p.m, p.nn, part + s * per_chunk + p.part, p.nn);
+    store_tile(acc, m0 + 16 * MT * (wave >> 1), c0 + 16 * NT * (wave & 1), p.m, p.nn, out + p.part, p.nn);
+}
+
+// Partial sums of both products over the rows of a chunk, in tiles of 32 M0 channels by 128 hidden columns and of 128 hidden
+// columns by 32 N1 channels.
+template <int M0, int N1, bool WHOLE>
+__global__ void __launch_bounds__(kFfnThreads, 2)
+k_ffn_dw_f32(DwSide<float> p0, DwSide<float> p1, int64_t n, int64_t chunk, int64_t per_chunk, float* __restrict__ part) {
+    __shared__ __attribute__((aligned(16))) uint8_t lds[ffn_lds<(M0 > N1 ? M0 : N1), 4>()];
+    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
+    const int tiles = p0.tiles + p1.tiles;
+    const int64_t s = u / tiles, r0 = s * chunk, rows = n - r0 < chunk ? n - r0 : chunk;
+    const int t = (int)(u - s * tiles);
+    if (t < p0.tiles) dw_tile_f32<M0, 4, WHOLE>(p0, t, r0, rows, lds, part + s * per_chunk);
+    else dw_tile_f32<4, N1, WHOLE>(p1, t - p0.tiles, r0, rows, lds, part + s * per_chunk);
 }
 
 // ---------------------------------------------------------------------------
@@ -670,8 +674,9 @@ static FfnLayout ffn_layout(int dtype, const FfnShape& d, bool bwd) {
         } else {
             L.m_nar = ffn_narrow(d.ci);
             L.n_nar = ffn_narrow(d.co);
-            bm0 = bm1 = L.m_nar ? 64 : 128;
-            bn0 = bn1 = L.n_nar ? 64 : 128;
+            bm0 = L.m_nar ? 64 : 128;
+            bn0 = bm1 = 128;
+            bn1 = L.n_nar ? 64 : 128;
         }
         L.tn0 = (int)ceil_div(2 * d.fp, bn0);
         L.t0 = (int)ceil_div(d.ci, bm0) * L.tn0;
@@ -694,14 +699,21 @@ template <typename T>
 static RowMat<const T> ffn_const(const RowMat<T>& m) { return {m.p, m.ld, m.gs, m.ts}; }
 
 // --- float32
-template <bool BKC>
+// f(WHOLE as a constant): the widths are multiples of four floats
+template <typename F>
+static void ffn_whole(const FfnShape& d, F f) {
+    if (d.ci % 4 == 0 && d.f % 4 == 0 && d.co % 4 == 0) f(std::true_type{});
+    else f(std::false_type{});
+}
+
+template <bool BKC, bool WHOLE>
 static void ffn_gemm_f32(RowMat<const float> A1, RowMat<const float> A2, int64_t n, int64_t k, const float* B1,
                          const float* B2, int64_t ldb, int co, float* Out, hipStream_t s) {
     const bool nar = ffn_narrow(co);
     const int nc = (int)ceil_div(co, nar ? 64 : 128);
     const bool sho = ffn_short(n, 128, nc);
-    auto* kern = sho ? (nar ? k_ffn_gemm_f32<BKC, 2, 2> : k_ffn_gemm_f32<BKC, 2, 4>)
-                     : (nar ? k_ffn_gemm_f32<BKC, 4, 2> : k_ffn_gemm_f32<BKC, 4, 4>);
+    auto* kern = sho ? (nar ? k_ffn_gemm_f32<BKC, 2, 2, WHOLE> : k_ffn_gemm_f32<BKC, 2, 4, WHOLE>)
+                     : (nar ? k_ffn_gemm_f32<BKC, 4, 2, WHOLE> : k_ffn_gemm_f32<BKC, 4, 4, WHOLE>);
     hipLaunchKernelGGL(kern, dim3((unsigned)(ceil_div(n, sho ? 64 : 128) * nc)), dim3(kFfnThreads), 0, s, A1, A2, n, k,
                        B1, B2, ldb, co, Out, nc);
 }
@@ -712,10 +724,13 @@ static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const float* X, const
     const RowMat<float> H = row_blocks(reinterpret_cast<float*>(ws + L.h), d.fp);
     const int nf = (int)ceil_div(d.f, 64);
     const bool sho = ffn_short(d.n, 128, nf);
-    auto* up = sho ? k_ffn_up_f32<2> : k_ffn_up_f32<4>;
-    hipLaunchKernelGGL(up, dim3((unsigned)(ceil_div(d.n, sho ? 64 : 128) * nf)), dim3(kFfnThreads), 0, s, X, d.n, d.ci, Wg,
-                       Wu, d.f, act, H, nf);
-    ffn_gemm_f32<false>(ffn_const(H), {}, d.n, d.f, Wd, nullptr, d.co, d.co, Y, s);
+    ffn_whole(d, [&](auto WHOLE) {
+        constexpr bool W = decltype(WHOLE)::value;
+        auto* up = sho ? k_ffn_up_f32<2, W> : k_ffn_up_f32<4, W>;
+        hipLaunchKernelGGL(up, dim3((unsigned)(ceil_div(d.n, sho ? 64 : 128) * nf)), dim3(kFfnThreads), 0, s, X, d.n, d.ci,
+                           Wg, Wu, d.f, act, H, nf);
+        ffn_gemm_f32<false, W>(ffn_const(H), {}, d.n, d.f, Wd, nullptr, d.co, d.co, Y, s);
+    });
 }
 
 static void ffn_bwd_rows(const FfnShape& d, const float* X, const float* Wg, const float* Wu, const float* Wd,
@@ -724,18 +739,24 @@ static void ffn_bwd_rows(const FfnShape& d, const float* X, const float* Wg, con
     if (ffn_res_f32(d)) return res_bwd(X, dY, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, (int)d.fp, H, dG, dU, dX, s);
     const int nf = (int)ceil_div(d.f, 64);
     const bool sho = ffn_short(d.n, 128, nf);
-    auto* mid = sho ? k_ffn_mid_f32<2> : k_ffn_mid_f32<4>;
-    hipLaunchKernelGGL(mid, dim3((unsigned)(ceil_div(d.n, sho ? 64 : 128) * nf)), dim3(kFfnThreads), 0, s, X, dY, d.n,
-                       d.ci, d.co, Wg, Wu, Wd, d.f, act, H, dG, dU, nf);
-    if (dX) ffn_gemm_f32<true>(ffn_const(dG), ffn_const(dU), d.n, d.f, Wg, Wu, d.f, d.ci, dX, s);
+    ffn_whole(d, [&](auto WHOLE) {
+        constexpr bool W = decltype(WHOLE)::value;
+        auto* mid = sho ? k_ffn_mid_f32<2, W> : k_ffn_mid_f32<4, W>;
+        hipLaunchKernelGGL(mid, dim3((unsigned)(ceil_div(d.n, sho ? 64 : 128) * nf)), dim3(kFfnThreads), 0, s, X, dY, d.n,
+                           d.ci, d.co, Wg, Wu, Wd, d.f, act, H, dG, dU, nf);
+        if (dX) ffn_gemm_f32<true, W>(ffn_const(dG), ffn_const(dU), d.n, d.f, Wg, Wu, d.f, d.ci, dX, s);
+    });
 }
 
-static void ffn_dw(const FfnLayout& L, const DwSide<float>& p0, const DwSide<float>& p1, int64_t n, float* part,
+static void ffn_dw(const FfnShape& d, const FfnLayout& L, const DwSide<float>& p0, const DwSide<float>& p1, float* part,
                    hipStream_t s) {
-    auto* kern = L.m_nar ? (L.n_nar ? k_ffn_dw_f32<2, 2> : k_ffn_dw_f32<2, 4>)
-                         : (L.n_nar ? k_ffn_dw_f32<4, 2> : k_ffn_dw_f32<4, 4>);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(L.chunks * (p0.tiles + p1.tiles))), dim3(kFfnThreads), 0, s, p0, p1, n,
-                       L.chunk, L.per_chunk, part);
+    ffn_whole(d, [&](auto WHOLE) {
+        constexpr bool W = decltype(WHOLE)::value;
+        auto* kern = L.m_nar ? (L.n_nar ? k_ffn_dw_f32<2, 2, W> : k_ffn_dw_f32<2, 4, W>)
+                             : (L.n_nar ? k_ffn_dw_f32<4, 2, W> : k_ffn_dw_f32<4, 4, W>);
+        hipLaunchKernelGGL(kern, dim3((unsigned)(L.chunks * (p0.tiles + p1.tiles))), dim3(kFfnThreads), 0, s, p0, p1, d.n,
+                           L.chunk, L.per_chunk, part);
+    });
 }
 
 // --- bfloat16
@@ -790,11 +811,11 @@ static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const uint16_t* X, co
     ffn_gemm_bf16<FB_MC>(ffn_const(H), {}, d.n, d.f, w.p, nullptr, w.ld, d.co, Y, s);
 }
 
-static void ffn_dw(const FfnLayout& L, const DwSide<uint16_t>& p0, const DwSide<uint16_t>& p1, int64_t n, float* part,
+static void ffn_dw(const FfnShape& d, const FfnLayout& L, const DwSide<uint16_t>& p0, const DwSide<uint16_t>& p1, float* part,
                    hipStream_t s) {
     auto* kern = L.m_nar ? (L.n_nar ? k_ffn_dw_bf16<4, true> : k_ffn_dw_bf16<4, false>)
                          : (L.n_nar ? k_ffn_dw_bf16<8, true> : k_ffn_dw_bf16<8, false>);
-    hipLaunchKernelGGL(kern, dim3((unsigned)(L.chunks * (p0.tiles + p1.tiles))), dim3(256), 0, s, p0, p1, n, L.chunk,
+    hipLaunchKernelGGL(kern, dim3((unsigned)(L.chunks * (p0.tiles + p1.tiles))), dim3(256), 0, s, p0, p1, d.n, L.chunk,
                        L.per_chunk, part);
 }
 
@@ -863,7 +884,7 @@ static void ffn_bwd(const FfnShape& d, const FfnLayout& L, const T* X, const T* 
     const bool up = dWg || dWu;
     const DwSide<T> p0{row_major(xs, ldx), ffn_const(dG), d.ci, (int)(2 * d.fp), L.tn0, up ? L.t0 : 0, 0};
     const DwSide<T> p1{ffn_const(H), row_major(ys, ldy), d.f, d.co, L.tn1, dWd ? L.t1 : 0, L.up};
-    if (n > 0) ffn_dw(L, p0, p1, n, part, s);
+    if (n > 0) ffn_dw(d, L, p0, p1, part, s);
     const int64_t total = dWd ? L.per_chunk : L.up;
     const int64_t blocks = ceil_div(total, kFfnThreads);
     hipLaunchKernelGGL(k_ffn_dw_sum<T>, dim3((unsigned)(blocks < 8192 ? blocks : 8192)), dim3(kFfnThreads), 0, s, part,

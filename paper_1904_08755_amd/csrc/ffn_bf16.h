@@ -27,9 +27,6 @@ namespace gsc {
 typedef __bf16 fbf16x8 __attribute__((ext_vector_type(8)));
 typedef short fs16x4 __attribute__((ext_vector_type(4)));
 
-constexpr int kFbBufFlags = 0x00020000;       // buffer descriptor word 3: 32-bit data format
-constexpr uint32_t kFbNone = 0x80000000u;     // an offset past any operand's end
-
 // s_waitcnt operand: vmcnt(n), the other counters left free (gfx9 encoding)
 template <int N>
 __device__ __forceinline__ void fb_wait() {
@@ -91,20 +88,20 @@ struct FbCopy {
                 first[j] = row;
                 in = col < s.rows;
             }
-            off[j] = in ? (uint32_t)((row >> 7) * s.m.ts + (row & 127) * s.m.ld + (col >> 5) * s.m.gs + (col & 31)) * 2 : kFbNone;
+            off[j] = in ? (uint32_t)((row >> 7) * s.m.ts + (row & 127) * s.m.ld + (col >> 5) * s.m.gs + (col & 31)) * 2 : kBufNone;
         }
     }
     // the step at reduction element k0 of K, into LDS at dst
     __device__ __forceinline__ void issue(const FbSide& s, int64_t k0, int64_t K, uint8_t* dst, int wave) const {
         const uint16_t* base = LAY == FB_KC ? s.m.at(0, k0).p : s.m.at(k0, 0).p;
         // an upper bound of the bytes from there on that may be read; what lies outside the operand is masked below
-        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, 0x7fffffff, kFbBufFlags);
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, 0x7fffffff, kBufFlags);
         const int left = (int)(K - k0 < 32 ? K - k0 : 32);   // (none from K on)
 #pragma unroll
         for (int j = 0; j < N; ++j)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(
                 rs, (__attribute__((address_space(3))) void*)(dst + (wave * N + j) * 1024), 16,
-                first[j] < left ? off[j] : kFbNone, 0, 0, 0);
+                first[j] < left ? off[j] : kBufNone, 0, 0, 0);
     }
 };
 

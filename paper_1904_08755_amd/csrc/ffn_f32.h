@@ -15,7 +15,7 @@ constexpr int kFfnBk = kFfnRowBytes / 4;
 
 // One side of a product: `rows` outputs by k reduction elements, element (r, k) at row r and column k of m (KC) or at
 // row k and column r (MC).  Rows and reduction elements behind the end read as 0.  SPLIT: the tile's rows
-// [0, R / 2) come from m and the others from p2, laid out alike (both from row 0 on).
+// [0, R / 2) come from m and the others from p2, laid out alike (both from row 0 on, `rows` of each).
 struct Side {
     RowMat<const float> m;
     const float* p2;
@@ -23,69 +23,67 @@ struct Side {
     int64_t k;
 };
 
-// A thread's share of a tile of R rows by one step, through registers into LDS.
-template <bool KC, int R, bool SPLIT>
+// The four floats from `bytes` behind a base that is the same for all lanes, `left` of them valid and the others 0, without
+// a branch (the compiler counts the loads in flight).  WHOLE: left is at most 0 or at least 4.
+template <bool WHOLE>
+__device__ __forceinline__ RowVec<float>::Raw get_f32(const float* base, uint32_t bytes, int64_t left) {
+    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, 0x7fffffff, kBufFlags);
+    if (WHOLE) return __builtin_amdgcn_raw_buffer_load_b128(rs, left > 0 ? bytes : kBufNone, 0, 0);
+    RowVec<float>::Raw r;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) r[e] = __builtin_amdgcn_raw_buffer_load_b32(rs, e < left ? bytes + 4 * e : kBufNone, 0, 0);
+    return r;
+}
+
+// A thread's share of a tile of R rows by one step, through registers into LDS.  Its pieces lie `DL` lines apart; SPLIT:
+// even ones in the tile's first half, odd ones in the other.  Offsets in bytes from the tile's first element of a step are
+// below 2^31 (128 rows of at most 2^20 floats).  WHOLE: no piece ends inside.
+template <bool KC, int R, bool SPLIT, bool WHOLE>
 struct TileCopy {
-    static constexpr int V = 4, BK = kFfnBk;
-    static constexpr int N = R * kFfnRowBytes / 16 / kFfnThreads;   // 16-byte pieces a thread
-    static constexpr int PER = KC ? BK / V : R / V;                 // pieces of a row (KC) or of a reduction element
-    static_assert(N >= 1 && kFfnThreads % PER == 0, "tile");
+    static_assert(!(KC && SPLIT), "only operands across the reduction are split");
+    static constexpr int V = 4, BK = kFfnBk, HALVES = SPLIT ? 2 : 1;
+    static constexpr int N = R * kFfnRowBytes / 16 / kFfnThreads;      // 16-byte pieces a thread
+    static constexpr int PER = KC ? BK / V : R / HALVES / V;           // pieces of a row (KC) or of a reduction element
+    static constexpr int DL = kFfnThreads / PER;
+    static_assert(N % HALVES == 0 && kFfnThreads % PER == 0, "tile");
     typedef RowVec<float>::Raw Raw;
 
-    RowMat<const float> m;  // from element (0, 0) of the thread's side on
+    RowMat<const float> m;
+    const float* p2;
     int line, at;       // first row (KC) or reduction element (MC), and the piece's first element across
-    int64_t across;     // MC: elements from `at` to the rows' end
+    int64_t across;     // MC: elements from `at` to the rows' end (of the half's first one)
     int lim;            // KC: valid lines
+    uint32_t off;       // the first piece's offset
     Raw r[N];
 
     __device__ __forceinline__ void start(const Side& s) {
-        const int c = threadIdx.x % PER;
         line = threadIdx.x / PER;
-        at = c * V;
+        at = threadIdx.x % PER * V;
         m = s.m;
-        if (KC) {
-            lim = (int)(s.rows < R ? s.rows : R);
-            across = 0;
-        } else {
-            int col = at;
-            if (SPLIT && at >= R / 2) {
-                m.p = s.p2;
-                col -= R / 2;
-            }
-            across = s.rows - col;
-            if (SPLIT && across > R / 2 - col) across = R / 2 - col;
-            m.p += (col >> 5) * m.gs + (col & 31);
-            lim = 0;
-        }
+        p2 = s.p2;
+        lim = (int)(s.rows < R ? s.rows : R);
+        across = s.rows - at;
+        off = (uint32_t)(KC ? line * m.ld + at : (at >> 5) * m.gs + (at & 31) + line * m.ld) * 4;
     }
     // the step at reduction element k0
     __device__ __forceinline__ void fetch(int64_t k0, int64_t k) {
-        constexpr int DL = kFfnThreads / PER;   // lines between a thread's pieces
-        if (KC) {
-            const float* b = m.p + (k0 >> 5) * m.gs + at;
-            const int64_t left = k - k0 - at;
+        const int64_t step = KC ? (k0 >> 5) * m.gs : (k0 >> 7) * m.ts + (k0 & 127) * m.ld;
+        const int64_t left = k - k0 - at;
+        const int kl = (int)(k - k0 < BK ? k - k0 : BK);
 #pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const int row = line + j * DL;
-                r[j] = load_vec<float, true>(b + (int64_t)row * m.ld, row < lim ? left : 0);
-            }
-        } else {
-            const float* b = m.p + (k0 >> 7) * m.ts + (k0 & 127) * m.ld;
-            const int kl = (int)(k - k0 < BK ? k - k0 : BK);
-#pragma unroll
-            for (int j = 0; j < N; ++j) {
-                const int kk = line + j * DL;
-                r[j] = load_vec<float, true>(b + (int64_t)kk * m.ld, kk < kl ? across : 0);
-            }
+        for (int j = 0; j < N; ++j) {
+            const int l = j / HALVES * DL;
+            const float* b = (SPLIT && (j & 1) ? p2 : m.p) + step + (int64_t)l * m.ld;
+            r[j] = get_f32<WHOLE>(b, off, KC ? (line + l < lim ? left : 0) : (line + l < kl ? across : 0));
         }
     }
     __device__ __forceinline__ void put(uint8_t* lds) const {
-        constexpr int DL = kFfnThreads / PER;
         const int c = threadIdx.x % PER;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
-            const int row = line + j * DL;
-            *reinterpret_cast<uint4*>(lds + place(row, c)) = uint4{r[j][0], r[j][1], r[j][2], r[j][3]};
+            const int row = line + j / HALVES * DL;
+            *reinterpret_cast<uint4*>(lds + place(row, c + (SPLIT && (j & 1) ? PER : 0))) =
+                uint4{r[j][0], r[j][1], r[j][2], r[j][3]};
         }
     }
     // Byte of piece c of a line.  KC: lines of 128 bytes, pieces permuted by the row modulo 8, so the
@@ -93,7 +91,7 @@ struct TileCopy {
     // 3 of the reduction element (a lane's q).
     static __device__ __forceinline__ int place(int row, int c) {
         if (KC) return row * kFfnRowBytes + ((c ^ (row & 7)) * 16);
-        constexpr int M = PER / 4 - 1;
+        constexpr int M = R / 16 - 1;
         return row * (R * 4) + (((c >> 2) ^ ((row >> 2) & 3 & M)) * 64) + (c & 3) * 16;
     }
 };
@@ -130,14 +128,15 @@ constexpr int ffn_lds() { return 2 * 32 * (MT + NT) * kFfnRowBytes; }
 // 16 NT wn .. (SPLIT: half of them from either half of the tile's columns).  The second operand goes
 // into the MFMA first, so lane (i, q) gets row 16 mi + i of its rows and four consecutive columns 4 q ..
 // of block ni.  LDS may be in use by other waves' earlier reads: starts with a barrier.
-template <bool AKC, bool BKC, int MT, int NT, bool SPLIT>
+// WHOLE: every width is a multiple of four floats.
+template <bool AKC, bool BKC, int MT, int NT, bool SPLIT, bool WHOLE>
 __device__ __forceinline__ void tile_product(const Side& A, const Side& B, uint8_t* lds, floatx4 (&acc)[MT][NT]) {
     constexpr int RA = 32 * MT, RB = 32 * NT, BK = kFfnBk;
     constexpr int STAGE = (RA + RB) * kFfnRowBytes;
     typedef Frag<AKC, RA> FA;
     typedef Frag<BKC, RB> FB;
-    TileCopy<AKC, RA, false> ca;
-    TileCopy<BKC, RB, SPLIT> cb;
+    TileCopy<AKC, RA, false, WHOLE> ca;
+    TileCopy<BKC, RB, SPLIT, WHOLE> cb;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
     const int64_t K = A.k;
     ca.start(A);

@@ -130,8 +130,8 @@ struct ResCopies {
         constexpr int L = O::loads(S);
         int& left = O::last(S) ? lasts : pairs;
         const uint8_t*& src = O::last(S) ? last : pair;
-        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)src, (short)0, 0x7fffffff, kFbBufFlags);
-        const uint32_t off = left > 0 ? (uint32_t)(wave * L * 1024 + (threadIdx.x & 63) * 16) : kFbNone;
+        const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)src, (short)0, 0x7fffffff, kBufFlags);
+        const uint32_t off = left > 0 ? (uint32_t)(wave * L * 1024 + (threadIdx.x & 63) * 16) : kBufNone;
 #pragma unroll
         for (int j = 0; j < L; ++j)
             __builtin_amdgcn_raw_ptr_buffer_load_lds(

@@ -12,24 +12,13 @@
 #include "ffn_res.h"
 
 #include "ffn_act.h"
+#include "ffn_f32.h"
 #include "ffn_mma.h"
 
 namespace gsc {
 
 constexpr int kR32Threads = 256;
 constexpr int kR32Rows = 128;
-
-// The four floats from `bytes` behind a base that is the same for all lanes, `left` of them valid and the others 0, without
-// a branch (the compiler counts the loads in flight).  WHOLE: left is at most 0 or at least 4.
-template <bool WHOLE>
-__device__ __forceinline__ RowVec<float>::Raw r32_get(const float* base, uint32_t bytes, int left) {
-    const __amdgpu_buffer_rsrc_t rs = __builtin_amdgcn_make_buffer_rsrc((void*)base, (short)0, 0x7fffffff, kFbBufFlags);
-    if (WHOLE) return __builtin_amdgcn_raw_buffer_load_b128(rs, left > 0 ? bytes : kFbNone, 0, 0);
-    RowVec<float>::Raw r;
-#pragma unroll
-    for (int e = 0; e < 4; ++e) r[e] = __builtin_amdgcn_raw_buffer_load_b32(rs, e < left ? bytes + 4 * e : kFbNone, 0, 0);
-    return r;
-}
 
 // A chunk of 32 hidden columns in LDS: K rows of 32 columns of Wg and of Wu, and 32 rows of K columns of Wd (K channels; zeros
 // behind the matrices' ends).  The 16-byte pieces of a row are permuted by the row modulo 8, so that 32 lanes
@@ -50,9 +39,9 @@ struct R32Chunk {
         for (int s = 0; s < N; ++s) {
             const int64_t at = (int64_t)(32 * s) * f + c0;
             const int left = (int)r + 32 * s < ci ? f - c0 - (int)c * 4 : 0;
-            g[s] = r32_get<WHOLE>(Wg + at, up, left);
-            u[s] = r32_get<WHOLE>(Wu + at, up, left);
-            d[s] = r32_get<WHOLE>(Wd + (int64_t)c0 * co + 32 * s, down, c0 + (int)r < f ? co - 32 * s - (int)c * 4 : 0);
+            g[s] = get_f32<WHOLE>(Wg + at, up, left);
+            u[s] = get_f32<WHOLE>(Wu + at, up, left);
+            d[s] = get_f32<WHOLE>(Wd + (int64_t)c0 * co + 32 * s, down, c0 + (int)r < f ? co - 32 * s - (int)c * 4 : 0);
         }
     }
     __device__ __forceinline__ void put(uint8_t* lds) const {
@@ -85,7 +74,7 @@ template <int K, bool WHOLE>
 __device__ __forceinline__ void r32_load(const float* m, int64_t rows, int c, int i, int q, floatx4 (&x)[K / 8]) {
 #pragma unroll
     for (int j = 0; j < K / 8; ++j) {
-        const RowVec<float>::Raw r = r32_get<WHOLE>(m + 8 * j, (uint32_t)(i * c + 4 * q) * 4, i < rows ? c - 8 * j - 4 * q : 0);
+        const RowVec<float>::Raw r = get_f32<WHOLE>(m + 8 * j, (uint32_t)(i * c + 4 * q) * 4, i < rows ? c - 8 * j - 4 * q : 0);
 #pragma unroll
         for (int e = 0; e < 4; ++e) x[j][e] = __uint_as_float(r[e]);
     }

@@ -43,6 +43,11 @@ struct RowVec<uint16_t> {
     }
 };
 
+// Buffer loads (a bounds check instead of a branch): word 3 of the descriptor for 32-bit data, and an offset past any
+// operand's end, which reads zeros.
+constexpr int kBufFlags = 0x00020000;
+constexpr uint32_t kBufNone = 0x80000000u;
+
 // Elements [0, left) of 16 bytes, zeros behind them.  TAIL = false: left is 0 or at least V.
 template <typename T, bool TAIL>
 __device__ __forceinline__ typename RowVec<T>::Raw load_vec(const T* p, int64_t left) {
