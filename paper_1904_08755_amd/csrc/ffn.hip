@@ -608,17 +608,22 @@ struct FfnLayout {
     int tn0, t0, tn1, t1;
 };
 
+// Whether tiles of 128 rows leave at most a quarter of their last round of compute units idle.
+static bool ffn_fills(int64_t n) {
+    const int64_t tiles = ceil_div(n, 128), cus = device_cus();
+    return 4 * tiles >= 3 * ceil_div(tiles, cus) * cus;
+}
+
 // Whether the kernels that keep rows in registers can take a bfloat16 call at all.
 static bool ffn_res_can(const FfnShape& d) { return d.ci <= kResMax && d.co <= kResMax; }
 
 // ... and do.  Forward, up to 128 channels: from about 100 tiles of 128 rows on (16,000 rows of 128 channels 20 us, tiles 21; of
 // 100 channels, which tiles have to copy first, 14 and 21; 8,000 rows of 128 channels 19 and 16).  Wider ones take a block a
-// compute unit: where the last round of blocks leaves less than a quarter of the device idle (256 channels: 30,000 rows 55
+// compute unit: where they fill their rounds (256 channels: 30,000 rows 55
 // and 61 us, 45,000 rows in a second round of 96 blocks 96 and 84, 60,000 rows 102 and 112).
 static bool ffn_res_fwd(const FfnShape& d) {
-    const int64_t tiles = ceil_div(d.n, 128), cus = device_cus();
     if (!ffn_res_can(d)) return false;
-    return d.ci <= 128 && d.co <= 128 ? tiles >= 100 : 4 * tiles >= 3 * ceil_div(tiles, cus) * cus;
+    return d.ci <= 128 && d.co <= 128 ? ceil_div(d.n, 128) >= 100 : ffn_fills(d.n);
 }
 // Backward: once H, dG and dU outgrow the 256 MB of the last-level cache, where the tiles' traffic costs more than their better
 // spread over the device saves (forward and backward of 128 channels, 512 hidden: 60,000 rows 155 us, tiles 148; 90,000 rows
@@ -627,18 +632,25 @@ static bool ffn_res_bwd(const FfnShape& d) {
     return ffn_res_can(d) && (d.ci > 64 || d.co > 64) && d.n * d.fp * 6 >= (int64_t)256 << 20;
 }
 
-static bool ffn_res_f32(const FfnShape& d) { return d.ci <= kResMaxF32 && d.co <= kResMaxF32 && d.n >= 8192; }
+// float32: where the blocks fill their rounds (64 channels, 256 hidden, forward and backward: 16,000 rows 119 us, tiles 95;
+// 32,000 rows 141 and 156; 45,000 rows 215 and 207; 60,000 rows 227 and 259); forward always up to 32 channels, which
+// are few products a chunk (1,000 rows 11.1 and 11.4 us, 45,000 rows 18 and 25).
+static bool ffn_res_f32(const FfnShape& d, bool bwd) {
+    if (d.ci > kResMaxF32 || d.co > kResMaxF32) return false;
+    return ffn_fills(d.n) || (!bwd && d.ci <= 32 && d.co <= 32);
+}
 
 // float32: tiles of 64 outputs instead of 128 in a direction where they leave less of the last one empty.
 static bool ffn_narrow(int64_t rows) { return ceil_div(rows, 64) % 2 == 1 && rows < 512; }
 
 // Row chunks of the weights' gradients: as many as fill the device once with two blocks a compute unit (a few blocks more
-// would take a second round: 1,032 blocks 605 us, 504 blocks 525 us), at least 512 rows each.
-constexpr int64_t kFfnChunkRows = 512;
+// would take a second round: 1,032 blocks 605 us, 504 blocks 525 us), of at least 512 rows, or 128 up to 32 chunks: few rows
+// leave the device to few blocks, whose length is what counts, many rows pay for each chunk's sums (backward pass, 64 channels,
+// 256 hidden float32: 1,000 rows 35 us in chunks of 128 and 52 of 512; bfloat16: 30,000 rows 50 and 45 us).
 static int64_t ffn_chunks(int64_t n, int64_t tiles) {
-    int64_t c = 512 / tiles;
-    const int64_t most = ceil_div(n, kFfnChunkRows);
-    if (c > most) c = most;
+    int64_t most = ceil_div(n, 128);
+    if (most > 32) most = ceil_div(n, 512) > 32 ? ceil_div(n, 512) : 32;
+    const int64_t c = 512 / tiles < most ? 512 / tiles : most;
     return c < 1 ? 1 : c;
 }
 
@@ -720,7 +732,7 @@ static void ffn_gemm_f32(RowMat<const float> A1, RowMat<const float> A2, int64_t
 
 static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const float* X, const float* Wg, const float* Wu,
                     const float* Wd, int act, float* Y, char* ws, hipStream_t s) {
-    if (ffn_res_f32(d)) return res_fwd(X, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, Y, s);
+    if (ffn_res_f32(d, false)) return res_fwd(X, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, Y, s);
     const RowMat<float> H = row_blocks(reinterpret_cast<float*>(ws + L.h), d.fp);
     const int nf = (int)ceil_div(d.f, 64);
     const bool sho = ffn_short(d.n, 128, nf);
@@ -736,7 +748,7 @@ static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const float* X, const
 static void ffn_bwd_rows(const FfnShape& d, const float* X, const float* Wg, const float* Wu, const float* Wd,
                          const float* dY, int act, float* dX, RowMat<float> H, RowMat<float> dG, RowMat<float> dU,
                          hipStream_t s) {
-    if (ffn_res_f32(d)) return res_bwd(X, dY, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, (int)d.fp, H, dG, dU, dX, s);
+    if (ffn_res_f32(d, true)) return res_bwd(X, dY, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, (int)d.fp, H, dG, dU, dX, s);
     const int nf = (int)ceil_div(d.f, 64);
     const bool sho = ffn_short(d.n, 128, nf);
     ffn_whole(d, [&](auto WHOLE) {

@@ -429,6 +429,25 @@ def test_gated_ffn_choices(i):
     assert all(torch.equal(p, q) for p, q in zip(gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, act), grads))
 
 
+# float32 rows in registers: one round of blocks filled and not, every width class, widths that are no multiples of four
+FFN_F32 = [(32700, 64, 256, 64, 0), (30001, 32, 64, 32, 1), (31000, 96, 100, 33, 0), (27001, 30, 67, 96, 1),
+           (26000, 128, 128, 128, 0), (33100, 128, 64, 100, 0), (30011, 101, 97, 7, 1), (700, 31, 70, 29, 1),
+           (130, 32, 64, 32, 0), (60001, 5, 9, 66, 0)]
+
+
+@pytest.mark.parametrize("i", range(len(FFN_F32)))
+def test_gated_ffn_float32(i):
+    n, ci, f, co, at = FFN_F32[i]
+    act = ACTS[i % len(ACTS)]
+    X, Wg, Wu, Wd, dY = _ffn_inputs(torch.float32, n, ci, f, co, at)
+    Y = gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd, act)
+    grads = gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, act)
+    _ffn_check(X, Wg, Wu, Wd, dY, act, Y, grads)
+    assert torch.equal(gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, act, need_dw=False)[0], grads[0])
+    dW = gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, act, need_dx=False)
+    assert dW[0] is None and all(torch.equal(p, q) for p, q in zip(dW[1:], grads[1:]))
+
+
 @BOTH
 @pytest.mark.parametrize("act", ACTS)
 @pytest.mark.parametrize("n", [2, 200])
