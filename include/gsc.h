@@ -614,9 +614,11 @@ int gsc_rotary(int32_t dtype, const void* X, int64_t n, int32_t heads, int32_t d
  *   RELU max(g, 0) (NaN passes through),  SIGMOID 1 / (1 + exp(-g)).
  * bfloat16: products on bfloat16 operands with float32 sums; the hidden rows
  * act(X Wg) * (X Wu) are rounded to bfloat16 once between the two products.
- * ws: gsc_gated_ffn_fwd_ws_bytes bytes (the hidden rows), aligned to 16 bytes,
- * contents not kept; calls that may overlap need one each.  Asynchronous.
- * Errors: EINVAL, ESHORT (ws), EHIP. */
+ * A row of X with a NaN or an infinity gives NaN or infinite values in that
+ * row alone.  ws: gsc_gated_ffn_fwd_ws_bytes bytes (hidden rows and, in
+ * bfloat16, laid out weights and copies of unaligned rows), aligned to 16 bytes,
+ * contents not kept; calls that may overlap need one each, and so does a
+ * captured graph.  Asynchronous.  Errors: EINVAL, ESHORT (ws), EHIP. */
 typedef enum {
     GSC_GATE_SILU = 0,
     GSC_GATE_GELU = 1,
@@ -638,7 +640,7 @@ int gsc_gated_ffn_fwd(int32_t dtype, const void* X, int64_t n, int32_t c_in, con
  * sums stay in float32 until the results are rounded; the weights' gradients
  * therefore carry no more digits than bfloat16's.  With n = 0 the weights'
  * gradients are 0.  ws: gsc_gated_ffn_bwd_ws_bytes bytes, aligned to 16 bytes,
- * contents not kept.  Asynchronous.  Errors: EINVAL, ESHORT (ws), EHIP. */
+ * contents not kept, one for each call that may overlap.  Asynchronous.  Errors: EINVAL, ESHORT (ws), EHIP. */
 size_t gsc_gated_ffn_bwd_ws_bytes(int32_t dtype, int64_t n, int32_t c_in, int32_t hidden, int32_t c_out);
 int gsc_gated_ffn_bwd(int32_t dtype, const void* X, int64_t n, int32_t c_in, const void* Wg, const void* Wu,
                       int32_t hidden, const void* Wd, int32_t c_out, const void* dY, int32_t act, void* dX, void* dWg,

@@ -27,6 +27,8 @@ namespace gsc {
 typedef __bf16 fbf16x8 __attribute__((ext_vector_type(8)));
 typedef short fs16x4 __attribute__((ext_vector_type(4)));
 
+constexpr int kFbStages = 3;
+
 // s_waitcnt operand: vmcnt(n), the other counters left free (gfx9 encoding)
 template <int N>
 __device__ __forceinline__ void fb_wait() {
@@ -227,15 +229,15 @@ __device__ __forceinline__ uint32_t fb_frag_mc(int t) {
 // acc += A B^T of a block of WM x WN waves, wave tiles of 16 MT rows by 16 NT columns.  PAIR: B's columns are two sides of
 // half as many each, the second one's rows at b2 (a wave takes half of its columns from either).  The second operand
 // goes into the MFMA first: lane (i, q) gets row 16 mi + i of its rows and four consecutive columns
-// 4 q .. of block ni.  lds: NS stages.  Every wave has passed its last read of lds before the call.
-template <int WM, int WN, int MT, int NT, int NS = 3>
+// 4 q .. of block ni.  lds: kFbStages stages.  Every wave has passed its last read of lds before the call.
+template <int WM, int WN, int MT, int NT>
 struct FbShape {
     static constexpr int NW = WM * WN, BM = 16 * MT * WM, BN = 16 * NT * WN;
     static constexpr int STAGE = (BM + BN) * 64;
-    static constexpr int LDS = NS * STAGE;
+    static constexpr int LDS = kFbStages * STAGE;
 };
 
-template <int WM, int WN, int MT, int NT, FbLay AL, FbLay BL, bool PAIR = false, int NS = 3>
+template <int WM, int WN, int MT, int NT, FbLay AL, FbLay BL, bool PAIR = false>
 __device__ __forceinline__ void fb_product(const FbSide& A, const FbSide& B, const uint16_t* b2, int64_t K, uint8_t* lds,
                                            floatx4 (&acc)[MT][NT]) {
     typedef FbShape<WM, WN, MT, NT> S;
@@ -274,15 +276,15 @@ __device__ __forceinline__ void fb_product(const FbSide& A, const FbSide& B, con
             fb[t] = fb_lds(lds) + CA::BYTES + (t < NT / 2 ? 0 : CB::BYTES) + fb_frag_mc<BL, RB>(NT / 2 * wn + t % (NT / 2));
     }
 #pragma unroll
-    for (int s = 0; s < NS - 1; ++s)
+    for (int s = 0; s < kFbStages - 1; ++s)
         if (s < steps) issue(s, s);
     int slot = 0;
     for (int s = 0; s < steps; ++s) {
-        if (s + NS - 2 < steps) fb_wait<LD * (NS - 2)>();
+        if (s + kFbStages - 2 < steps) fb_wait<LD * (kFbStages - 2)>();
         else fb_wait<0>();
         fb_barrier();
-        const int into = slot == 0 ? NS - 1 : slot - 1;   // the stage of step s - 1
-        if (s + NS - 1 < steps) issue(s + NS - 1, into);
+        const int into = slot == 0 ? kFbStages - 1 : slot - 1;   // the stage of step s - 1
+        if (s + kFbStages - 1 < steps) issue(s + kFbStages - 1, into);
         fbf16x8 a[MT], b[NT];
         const uint32_t at = (uint32_t)(slot * S::STAGE);
         if constexpr (BL == FB_KC) {
@@ -305,7 +307,7 @@ __device__ __forceinline__ void fb_product(const FbSide& A, const FbSide& B, con
 #pragma unroll
             for (int ni = 0; ni < NT; ++ni)
                 acc[mi][ni] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b[ni], a[mi], acc[mi][ni], 0, 0, 0);
-        slot = slot == NS - 1 ? 0 : slot + 1;
+        slot = slot == kFbStages - 1 ? 0 : slot + 1;
     }
 }
 
