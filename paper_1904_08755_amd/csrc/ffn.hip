@@ -4,21 +4,21 @@
 //   dH = dY Wd^T,  dG = dH U act'(G),  dU = dH act(G)
 //   dX = dG Wg^T + dU Wu^T,  dWg = X^T dG,  dWu = X^T dU,  dWd = H^T dY
 //
-// Products run on the matrix cores (v_mfma_f32_16x16x32_bf16, v_mfma_f32_16x16x4f32) with float32
-// sums.  The forward pass is two kernels: both projections with the activation and the product
-// (k_ffn_up: G and U never leave the registers), then the output projection (k_ffn_gemm).  The
-// backward pass works G and U out again from X (a third more products than reading them back, but the
-// forward pass need not write them nor the program keep them: at 256 channels and 1,024 hidden
-// ones their two arrays would be eight times the bytes of X): k_ffn_mid computes G, U and dH of a tile and
-// stores H, dG and dU; k_ffn_gemm adds dX; k_ffn_dw adds the weights' gradients over row chunks and
-// k_ffn_dw_sum adds the chunks in order, so that every result is bit-reproducible.
+// Products run on the matrix cores with float32 sums.  The backward pass works G and U out again from X (a third more products
+// than reading them back, but the forward pass need not write them nor the program keep them: at 256 channels and 1,024
+// hidden ones their two arrays would be eight times the bytes of X).  Which kernels take a call:
+//   a few rows           k_ffn_few, twice;
+//   many rows, narrow    rows stay in registers while the weights pass through LDS (ffn_res.hip, ffn_res_f32.hip);
+//   else                 tiles: k_ffn_up (both projections with the activation; G and U never leave the registers) and
+//                        k_ffn_gemm; backward k_ffn_mid (G, U and dH of a tile; stores H, dG and dU) and k_ffn_gemm for dX.
+// The weights' gradients are k_ffn_dw over row chunks and k_ffn_dw_sum, which adds the chunks in order: every result is
+// bit-reproducible.
 //
-// bfloat16: G, U, dH and all sums stay in float32; H, dG and dU are rounded to bfloat16 once, as the
-// matrix cores take them, and the results once as they are stored.  Its tiles copy operands straight
-// into LDS (ffn_bf16.h), which takes rows of whole 16-byte pieces at 16-byte addresses: operands that are not
-// are copied into the workspace first, their rows padded with zeros (k_ffn_pad; the weights and at
-// most three passes over rows, against kernels that would load element by element).  float32 tiles
-// (ffn_f32.h) take any address.
+// bfloat16: G, U, dH and all sums stay in float32; H, dG and dU are rounded to bfloat16 once, as the matrix cores take them, and
+// the results once as they are stored.  Its tiles copy operands straight into LDS (ffn_bf16.h), which takes rows of whole
+// 16-byte pieces at 16-byte addresses: operands that are not are copied into the workspace first, their rows padded with zeros
+// (k_ffn_pad; the weights and at most two passes over rows, against kernels that would load element by element).  float32
+// tiles (ffn_f32.h) take any address.
 #include "ffn_act.h"
 #include "ffn_bf16.h"
 #include "ffn_f32.h"
@@ -229,7 +229,8 @@ __device__ __forceinline__ void dw_tile_f32(const DwSide<float>& p, int t, int64
 }
 
 // Partial sums of both products over the rows of a chunk, in tiles of 32 M0 channels by 128 hidden columns and of 128 hidden
-// columns by 32 N1 channels.
+// columns by 32 N1 channels.  120,011 rows, 64 channels, 256 hidden: 145 us (tiles of 64 x 64: 166), the matrix cores
+// busy 59 % of it; more blocks change nothing, what counts is the 447 MB from beyond the L2s.
 template <int M0, int N1, bool WHOLE>
 __global__ void __launch_bounds__(kFfnThreads, 2)
 k_ffn_dw_f32(DwSide<float> p0, DwSide<float> p1, int64_t n, int64_t chunk, int64_t per_chunk, float* __restrict__ part) {
@@ -271,7 +272,8 @@ __global__ void __launch_bounds__(kFfnThreads) k_ffn_pad(FfnPad p) {
             }
         const int64_t row = at / (ld / 8);
         const int c = (int)(at - row * (ld / 8)) * 8;
-        const RowVec<uint16_t>::Raw v = load_vec<uint16_t, true>(src + row * cols + c, cols - c);
+        const RowVec<uint16_t>::Raw v = cols < 8 ? load_vec<uint16_t, true>(src + row * cols + c, cols - c)
+                                                 : load_last(src + row * cols, c, cols);
         *reinterpret_cast<uint4*>(dst + at * 8) = uint4{v[0], v[1], v[2], v[3]};
     }
 }
@@ -619,8 +621,8 @@ static bool ffn_res_can(const FfnShape& d) { return d.ci <= kResMax && d.co <= k
 
 // ... and do.  Forward, up to 128 channels: from about 100 tiles of 128 rows on (16,000 rows of 128 channels 20 us, tiles 21; of
 // 100 channels, which tiles have to copy first, 14 and 21; 8,000 rows of 128 channels 19 and 16).  Wider ones take a block a
-// compute unit: where they fill their rounds (256 channels: 30,000 rows 55
-// and 61 us, 45,000 rows in a second round of 96 blocks 96 and 84, 60,000 rows 102 and 112).
+// compute unit: where they fill their rounds (256 channels: 30,000 rows 55 and 61 us, 45,000 rows in a second round of 96
+// blocks 96 and 84, 60,000 rows 102 and 112).
 static bool ffn_res_fwd(const FfnShape& d) {
     if (!ffn_res_can(d)) return false;
     return d.ci <= 128 && d.co <= 128 ? ceil_div(d.n, 128) >= 100 : ffn_fills(d.n);

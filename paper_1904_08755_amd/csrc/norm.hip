@@ -69,17 +69,7 @@ __device__ __forceinline__ void load_row(const T* x, int l, int c, typename RowV
         const int col = (i * LPR + l) * V;
         if (ln_whole<NV>(i)) raw[i] = *reinterpret_cast<const Raw*>(x + col);
         else if (!TAIL || c < V) raw[i] = load_vec<T, TAIL>(x + col, c - col);
-        else {
-            Raw r = {0, 0, 0, 0};
-            if (col < c) r = *reinterpret_cast<const Raw*>(x + (col + V <= c ? col : c - V));
-            if (col + V > c) {
-                const int sh = (V - c % V) * 8 * (int)sizeof(T);   // 16 .. 112 bits, the same for all lanes
-                const uint64_t lo = (uint64_t)r[1] << 32 | r[0], hi = (uint64_t)r[3] << 32 | r[2];
-                const uint64_t a = sh >= 64 ? hi >> (sh - 64) : lo >> sh | hi << (64 - sh), b = sh >= 64 ? 0 : hi >> sh;
-                r = Raw{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
-            }
-            raw[i] = r;
-        }
+        else raw[i] = load_last<T>(x, col, c);
     }
 }
 // ... and back: the partial piece in stores of 8, 4 and 2 bytes.

@@ -68,6 +68,23 @@ __device__ __forceinline__ typename RowVec<T>::Raw load_vec(const T* p, int64_t 
     return r;
 }
 
+// Elements [col, col + V) of a row of c >= V, zeros behind its end.  A piece that the end cuts is the row's last 16 bytes,
+// shifted by as much in every lane (loads of its elements one by one take as long as the rest of a row).
+template <typename T>
+__device__ __forceinline__ typename RowVec<T>::Raw load_last(const T* x, int64_t col, int c) {
+    constexpr int V = RowVec<T>::V;
+    typedef typename RowVec<T>::Raw Raw;
+    Raw r = {0, 0, 0, 0};
+    if (col < c) r = *reinterpret_cast<const Raw*>(x + (col + V <= c ? col : c - V));
+    if (col + V > c) {
+        const int sh = (V - c % V) * 8 * (int)sizeof(T);   // 16 .. 112 bits (where col < c)
+        const uint64_t lo = (uint64_t)r[1] << 32 | r[0], hi = (uint64_t)r[3] << 32 | r[2];
+        const uint64_t a = sh >= 64 ? hi >> (sh & 63) : lo >> sh | hi << (64 - sh), b = sh >= 64 ? 0 : hi >> sh;
+        r = Raw{(uint32_t)a, (uint32_t)(a >> 32), (uint32_t)b, (uint32_t)(b >> 32)};
+    }
+    return r;
+}
+
 template <typename T, bool TAIL>
 __device__ __forceinline__ void store_vec(T* p, int64_t left, const float (&v)[RowVec<T>::V]) {
     typedef RowVec<T> R;

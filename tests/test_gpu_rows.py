@@ -114,6 +114,21 @@ def test_layer_norm_shapes(dtype, n, c, at, weights):
         assert torch.equal(out[0], dX) and torch.equal(out[1], dgamma)
 
 
+@BOTH
+@pytest.mark.parametrize("c", [9, 10, 11, 12, 13, 14, 15, 130, 515, 1025, 1026, 1029, 1030, 1031, 1801])
+def test_layer_norm_row_ends(dtype, c):
+    """Every length of a row's last piece, at any address, and the rows behind it untouched."""
+    test_layer_norm_shapes(dtype, 67, c, c % 3, True)
+    g = _gen(c, 5)
+    X, dY = _randn(g, 9, c, dtype=dtype), _randn(g, 9, c, dtype=dtype)
+    buf = torch.full((11 * c,), 7.0, dtype=dtype, device=DEV)
+    _, mean, rstd = gsc.gsc_layer_norm_fwd(X, Y=buf[c:10 * c].view(9, c))
+    assert (buf[:c] == 7).all() and (buf[10 * c:] == 7).all()
+    buf.fill_(7.0)
+    gsc.gsc_layer_norm_bwd(X, dY, mean, rstd, dX=buf[c:10 * c].view(9, c))
+    assert (buf[:c] == 7).all() and (buf[10 * c:] == 7).all()
+
+
 @pytest.mark.parametrize("c", [1, 24, 300, 2048, 3000])
 def test_layer_norm_offset_and_constant_rows(c):
     """A large common offset costs no digits of the variance; a constant row normalises to beta."""
