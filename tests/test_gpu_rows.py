@@ -547,6 +547,18 @@ def test_gated_ffn_past_32_bits():
         _ffn_check(x, Wg, Wu, Wd, dy, "silu", Y[sl].contiguous(), (dX[sl].contiguous(), None, None, None))
 
 
+@pytest.mark.parametrize("dtype,n,ci,f,co", [(torch.bfloat16, (1 << 23) + 77, 256, 64, 256),
+                                             (torch.float32, (1 << 24) + 133, 64, 64, 64),
+                                             (torch.float32, (1 << 21) + 77, 8, 1040, 8)])
+def test_gated_ffn_past_32_bits_rows_in_registers(dtype, n, ci, f, co):
+    """Rows, or hidden rows, of more than 2^32 bytes; the first and last rows against a call on them alone."""
+    X, Wg, Wu, Wd, dY = _ffn_inputs(dtype, n, ci, f, co)
+    Y, dX = gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd), gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, need_dw=False)[0]
+    for sl in (slice(0, 200), slice(n - 200, n)):
+        x, dy = X[sl].contiguous(), dY[sl].contiguous()
+        _ffn_check(x, Wg, Wu, Wd, dy, "silu", Y[sl].contiguous(), (dX[sl].contiguous(), None, None, None))
+
+
 # --------------------------------------------------------------------------- #
 # streams, graphs, refusals, and all of them together
 # --------------------------------------------------------------------------- #
@@ -613,6 +625,33 @@ def test_rows_two_streams(dtype):
     assert torch.equal(Y, want[0][0]) and torch.equal(R, want[0][3]) and torch.equal(Z, want[0][4])
     assert all(torch.equal(p, q) for p, q in zip(grads[1:], want[0][5:8]))
     assert torch.equal(sums[1], gsc.gsc_layer_norm_bwd(X, dY, mean, rstd, gamma)[1])
+
+
+@pytest.mark.parametrize("dtype,n,ci,f,co", [(torch.bfloat16, 13000, 128, 128, 128), (torch.bfloat16, 30000, 200, 1600, 256),
+                                             (torch.float32, 32001, 64, 128, 64), (torch.bfloat16, 13000, 99, 130, 64)])
+def test_gated_ffn_streams_and_graph_many_rows(dtype, n, ci, f, co):
+    """The kernels that keep rows in registers: two at once on streams of their own, and captured and replayed."""
+    sets = [_ffn_inputs(dtype, n, ci, f, co, key=key) for key in (1, 2)]
+    both = lambda X, Wg, Wu, Wd, dY: [gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd), *gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY)]
+    want = [both(*s) for s in sets]
+    torch.cuda.synchronize()
+    streams, got = [torch.cuda.Stream(), torch.cuda.Stream()], [None, None]
+    for i, s in enumerate(streams):
+        with torch.cuda.stream(s):
+            got[i] = both(*sets[i])
+    torch.cuda.synchronize()
+    assert all(torch.equal(p, q) for w, o in zip(want, got) for p, q in zip(w, o))
+    ins = [t.clone() for t in sets[0]]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        outs = both(*ins)
+    for i in (1, 0, 1):
+        for t, new in zip(ins, sets[i]):
+            t.copy_(new)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(outs, want[i]))
+        both(*sets[0])
 
 
 def test_rows_refusals():
