@@ -851,7 +851,8 @@ static void ffn_fwd_few(const FfnShape& d, const FfnLayout& L, const T* X, const
     constexpr int W = kFewCols * (16 / (int)sizeof(T));
     float* H = reinterpret_cast<float*>(ws + L.h);
     const int n = (int)d.n;
-    auto* up = n == 1 ? k_ffn_few<T, T, float, 1, true> : (n == 2 ? k_ffn_few<T, T, float, 2, true> : k_ffn_few<T, T, float, 4, true>);
+    auto* up = n == 1 ? k_ffn_few<T, T, float, 1, true>
+                      : (n == 2 ? k_ffn_few<T, T, float, 2, true> : k_ffn_few<T, T, float, 4, true>);
     auto* down = n == 1 ? k_ffn_few<float, T, T, 1, false>
                         : (n == 2 ? k_ffn_few<float, T, T, 2, false> : k_ffn_few<float, T, T, 4, false>);
     const int threads = n <= 2 ? few_threads<1>() : few_threads<4>();

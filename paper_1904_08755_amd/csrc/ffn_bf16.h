@@ -118,21 +118,21 @@ __device__ __forceinline__ fbf16x8 fb_join(fs16x4 lo, fs16x4 hi) {
 
 // Four or eight KC blocks of A at a (1 KiB apart) with two or four KC blocks of B at b.
 __device__ __forceinline__ void fb_read_kk(uint32_t a, uint32_t b, fbf16x8 (&A)[4], fbf16x8 (&B)[2]) {
-    asm volatile(FB_R(4, 7, 0) FB_R(5, 7, 1024) FB_R(0, 6, 0) FB_R(1, 6, 1024) FB_R(2, 6, 2048) FB_R(3, 6, 3072) FB_WAIT
+    asm volatile(FB_R(4, 7, 0) FB_R(5, 7, 1024) FB_R(0, 6, 0) FB_R(1, 6, 1024) FB_R(2, 6, 2048) FB_R(3, 6, 3 * 1024) FB_WAIT
                  : "=&v"(A[0]), "=&v"(A[1]), "=&v"(A[2]), "=&v"(A[3]), "=&v"(B[0]), "=&v"(B[1])
                  : "v"(a), "v"(b)
                  : "memory");
 }
 __device__ __forceinline__ void fb_read_kk(uint32_t a, uint32_t b, fbf16x8 (&A)[4], fbf16x8 (&B)[4]) {
-    asm volatile(FB_R(4, 9, 0) FB_R(5, 9, 1024) FB_R(6, 9, 2048) FB_R(7, 9, 3072) FB_R(0, 8, 0) FB_R(1, 8, 1024)
-                     FB_R(2, 8, 2048) FB_R(3, 8, 3072) FB_WAIT
+    asm volatile(FB_R(4, 9, 0) FB_R(5, 9, 1024) FB_R(6, 9, 2048) FB_R(7, 9, 3 * 1024) FB_R(0, 8, 0) FB_R(1, 8, 1024)
+                     FB_R(2, 8, 2048) FB_R(3, 8, 3 * 1024) FB_WAIT
                  : "=&v"(A[0]), "=&v"(A[1]), "=&v"(A[2]), "=&v"(A[3]), "=&v"(B[0]), "=&v"(B[1]), "=&v"(B[2]), "=&v"(B[3])
                  : "v"(a), "v"(b)
                  : "memory");
 }
 __device__ __forceinline__ void fb_read_kk(uint32_t a, uint32_t b, fbf16x8 (&A)[8], fbf16x8 (&B)[4]) {
-    asm volatile(FB_R(8, 13, 0) FB_R(9, 13, 1024) FB_R(10, 13, 2048) FB_R(11, 13, 3072) FB_R(0, 12, 0) FB_R(1, 12, 1024)
-                     FB_R(2, 12, 2048) FB_R(3, 12, 3072) FB_R(4, 12, 4096) FB_R(5, 12, 5120) FB_R(6, 12, 6144)
+    asm volatile(FB_R(8, 13, 0) FB_R(9, 13, 1024) FB_R(10, 13, 2048) FB_R(11, 13, 3 * 1024) FB_R(0, 12, 0) FB_R(1, 12, 1024)
+                     FB_R(2, 12, 2048) FB_R(3, 12, 3 * 1024) FB_R(4, 12, 4096) FB_R(5, 12, 5120) FB_R(6, 12, 6144)
                          FB_R(7, 12, 7168) FB_WAIT
                  : "=&v"(A[0]), "=&v"(A[1]), "=&v"(A[2]), "=&v"(A[3]), "=&v"(A[4]), "=&v"(A[5]), "=&v"(A[6]),
                    "=&v"(A[7]), "=&v"(B[0]), "=&v"(B[1]), "=&v"(B[2]), "=&v"(B[3])
@@ -145,7 +145,7 @@ __device__ __forceinline__ void fb_read_km(uint32_t a, const uint32_t (&b)[4], f
     fs16x4 r[8];
     asm volatile(FB_T(4, 13, "0") FB_T(5, 13, "%17") FB_T(6, 14, "0") FB_T(7, 14, "%17") FB_T(8, 15, "0")
                      FB_T(9, 15, "%17") FB_T(10, 16, "0") FB_T(11, 16, "%17") FB_R(0, 12, 0) FB_R(1, 12, 1024)
-                         FB_R(2, 12, 2048) FB_R(3, 12, 3072) FB_WAIT
+                         FB_R(2, 12, 2048) FB_R(3, 12, 3 * 1024) FB_WAIT
                  : "=&v"(A[0]), "=&v"(A[1]), "=&v"(A[2]), "=&v"(A[3]), "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]),
                    "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
                  : "v"(a), "v"(b[0]), "v"(b[1]), "v"(b[2]), "v"(b[3]), "n"(STEP)
@@ -158,7 +158,7 @@ __device__ __forceinline__ void fb_read_km(uint32_t a, const uint32_t (&b)[4], f
     fs16x4 r[8];
     asm volatile(FB_T(8, 17, "0") FB_T(9, 17, "%21") FB_T(10, 18, "0") FB_T(11, 18, "%21") FB_T(12, 19, "0")
                      FB_T(13, 19, "%21") FB_T(14, 20, "0") FB_T(15, 20, "%21") FB_R(0, 16, 0) FB_R(1, 16, 1024)
-                         FB_R(2, 16, 2048) FB_R(3, 16, 3072) FB_R(4, 16, 4096) FB_R(5, 16, 5120) FB_R(6, 16, 6144)
+                         FB_R(2, 16, 2048) FB_R(3, 16, 3 * 1024) FB_R(4, 16, 4096) FB_R(5, 16, 5120) FB_R(6, 16, 6144)
                              FB_R(7, 16, 7168) FB_WAIT
                  : "=&v"(A[0]), "=&v"(A[1]), "=&v"(A[2]), "=&v"(A[3]), "=&v"(A[4]), "=&v"(A[5]), "=&v"(A[6]),
                    "=&v"(A[7]), "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]),

@@ -90,8 +90,8 @@ __device__ __forceinline__ void r32_here(floatx4 (&x)[K / 8]) {
     for (int j = 0; j < K / 8; ++j) asm volatile("" : "+v"(x[j]));
 }
 
-// A 32 x 32 tile to `rows` rows of `cols` columns at out (ALL: to all of them).  Lanes i and i + 16 exchange pieces (permlane16_swap), so that
-// a store covers 16 rows by 64 bytes.
+// A 32 x 32 tile to `rows` rows of `cols` columns at out (ALL: to all of them).  Lanes i and i + 16 exchange pieces
+// (permlane16_swap), so that a store covers 16 rows by 64 bytes.
 template <bool ALL>
 __device__ __forceinline__ void r32_store(float* out, int64_t ld, int64_t rows, int64_t cols, const floatx16& v) {
     typedef RowVec<float>::Raw Raw;
@@ -198,8 +198,8 @@ k_ffn_fwd_rows(const float* __restrict__ X, int64_t n, int ci, const float* __re
 template <int K, bool WHOLE, int ACT>
 __global__ void __launch_bounds__(kR32Threads, K <= 64 ? 2 : 1)
 k_ffn_bwd_rows(const float* __restrict__ X, const float* __restrict__ dY, int64_t n, int ci, const float* __restrict__ Wg,
-               const float* __restrict__ Wu, int f, const float* __restrict__ Wd, int co, int fp, RowMat<float> H, RowMat<float> dG,
-               RowMat<float> dU, float* __restrict__ dX) {
+               const float* __restrict__ Wu, int f, const float* __restrict__ Wd, int co, int fp, RowMat<float> H,
+               RowMat<float> dG, RowMat<float> dU, float* __restrict__ dX) {
     typedef R32Chunk<K, WHOLE> C;
     __shared__ __attribute__((aligned(16))) uint8_t lds[C::kBytes];
     const int i = threadIdx.x & 31, q = (threadIdx.x & 63) >> 5;

@@ -385,8 +385,8 @@ static void ln_fwd(const void* X_, int64_t n, int c, const float* gamma, const f
     ln_dispatch<T, 3>(c, [&](auto LPR, auto NV, auto TAIL) {
         constexpr int L = decltype(LPR)::value, N = decltype(NV)::value;
         auto* kern = k_ln_fwd<T, L, N, decltype(TAIL)::value>;
-        hipLaunchKernelGGL(kern, dim3((unsigned)ln_row_blocks(n, kLnThreads / L, ln_most(c, N * RowVec<T>::V, kLnFwdBlocks))), dim3(kLnThreads), 0, s,
-                           X, n, c, gamma, beta, eps, Y, mean, rstd);
+        const int64_t blocks = ln_row_blocks(n, kLnThreads / L, ln_most(c, N * RowVec<T>::V, kLnFwdBlocks));
+        hipLaunchKernelGGL(kern, dim3((unsigned)blocks), dim3(kLnThreads), 0, s, X, n, c, gamma, beta, eps, Y, mean, rstd);
     });
 }
 
