@@ -204,68 +204,57 @@ k_ffn_mid_res(const uint16_t* __restrict__ X, const uint16_t* __restrict__ dY, i
         pu[e] = g * a;
     };
     // array k of the chunk before, as bfloat16 pairs
-    auto put = [&](int k, int ch, bool in) {
+    auto put = [&](int k, int ch) {
 #pragma unroll
         for (int e = 0; e < 8; ++e)
             ph[e] = k == 0 ? pack_bf16(pd[2 * e], pd[2 * e + 1])
                            : (k == 1 ? pack_bf16(pg[2 * e], pg[2 * e + 1]) : pack_bf16(pu[2 * e], pu[2 * e + 1]));
-        // the wave's 32 rows of a block of 128 rows by 32 columns
-        uint16_t* out = (k == 0 ? H : (k == 1 ? dG : dU)).at(r0, (int64_t)(ch0 + ch) * 64 + 32 * wn).p;
-        if (in) res_store<true>(out, 32, 0, n - r0, 0, 32, ph);
-        else res_store<false>(out, 32, 0, n - r0, 0, 32, ph);
+        // the wave's 32 rows of a block of 128 rows by 32 columns (rows behind the last one too: the blocks are whole)
+        res_store<true>((k == 0 ? H : (k == 1 ? dG : dU)).at(r0, (int64_t)(ch0 + ch) * 64 + 32 * wn).p, 32, 0, 0, 0, 32, ph);
     };
-    // WHOLE: all of the wave's rows exist, and six stores follow the start of every chunk's last stage, so that the waits can
-    // count them (before the first chunk, and in it, they write zeros where its values come later).
-    auto run = [&](auto WHOLE) {
-        constexpr bool in = decltype(WHOLE)::value;
-        if (in) {
+    // Six stores follow the start of every chunk's last stage, so that the waits can count them: before the first chunk, and in
+    // it, they write where its values come later.
 #pragma unroll
-            for (int k = 0; k < 3; ++k) put(k, 0, true);
-        }
-        for (int cb = 0; cb < chunks; cb += O::U)
-            res_each<O::U>([&](auto UU) {
-                constexpr int u = decltype(UU)::value;
-                const int ch = cb + u;
-                if (ch >= chunks) return;
-                floatx16 g{}, up{}, dh{};
-                res_each<O::PS>([&](auto P) {
-                    constexpr int p = decltype(P)::value, S = u * O::SPC + p, E = 16 / O::PS / (2 * O::KP / 4);
-                    cp.template wait<S, in ? 6 : 0>();
-                    cp.template start<S + O::SLOTS - 1>(slot(std::integral_constant<int, S + O::SLOTS - 1>{}));
-                    const uint8_t* b = slot(std::integral_constant<int, S>{}) + wn * 2048;
-                    res_stream<2 * O::KP, 4, 7>(
-                        [&](int j) { return res_frag(b + (j >> 1) * 4096 + (j & 1) * 1024); },
-                        [&](int j, fbf16x8 w) {
-                            if (j & 1) up = res_mma(w, x[p * O::KP + (j >> 1)], up);
-                            else g = res_mma(w, x[p * O::KP + (j >> 1)], g);
-                        },
-                        [&](auto I) {
-#pragma unroll
-                            for (int e = 0; e < E; ++e) epi(p * (16 / O::PS) + decltype(I)::value * E + e);
-                        });
-                });
-                constexpr int S = u * O::SPC + O::PS;
-                cp.template wait<S, in && O::PS == 1 ? 6 : 0>();
+    for (int k = 0; k < 3; ++k) put(k, 0);
+    for (int cb = 0; cb < chunks; cb += O::U)
+        res_each<O::U>([&](auto UU) {
+            constexpr int u = decltype(UU)::value;
+            const int ch = cb + u;
+            if (ch >= chunks) return;
+            floatx16 g{}, up{}, dh{};
+            res_each<O::PS>([&](auto P) {
+                constexpr int p = decltype(P)::value, S = u * O::SPC + p, E = 16 / O::PS / (2 * O::KP / 4);
+                cp.template wait<S, 6>();
                 cp.template start<S + O::SLOTS - 1>(slot(std::integral_constant<int, S + O::SLOTS - 1>{}));
-                const uint8_t* b = slot(std::integral_constant<int, S>{}) + wn * 1024;
-                if (in || ch > 0) {
+                const uint8_t* b = slot(std::integral_constant<int, S>{}) + wn * 2048;
+                res_stream<2 * O::KP, 4, 7>(
+                    [&](int j) { return res_frag(b + (j >> 1) * 4096 + (j & 1) * 1024); },
+                    [&](int j, fbf16x8 w) {
+                        if (j & 1) up = res_mma(w, x[p * O::KP + (j >> 1)], up);
+                        else g = res_mma(w, x[p * O::KP + (j >> 1)], g);
+                    },
+                    [&](auto I) {
 #pragma unroll
-                    for (int k = 0; k < 3; ++k) put(k, ch > 0 ? ch - 1 : 0, in);
-                }
-                res_stream<KT, 4, 0>([&](int j) { return ResPairFrag{res_frag(b + j * 2048), res_frag(dyw + j * 1024)}; },
-                                     [&](int j, const ResPairFrag& w) { dh = res_mma(w.a, w.b, dh); }, [](auto) {});
-                pg = g;
-                pu = up;
-                pd = dh;
+                        for (int e = 0; e < E; ++e) epi(p * (16 / O::PS) + decltype(I)::value * E + e);
+                    });
             });
-    };
-    if (r0 + 32 <= n) run(std::true_type{});
-    else run(std::false_type{});
+            constexpr int S = u * O::SPC + O::PS;
+            cp.template wait<S, O::PS == 1 ? 6 : 0>();
+            cp.template start<S + O::SLOTS - 1>(slot(std::integral_constant<int, S + O::SLOTS - 1>{}));
+            const uint8_t* b = slot(std::integral_constant<int, S>{}) + wn * 1024;
+#pragma unroll
+            for (int k = 0; k < 3; ++k) put(k, ch > 0 ? ch - 1 : 0);
+            res_stream<KT, 4, 0>([&](int j) { return ResPairFrag{res_frag(b + j * 2048), res_frag(dyw + j * 1024)}; },
+                                 [&](int j, const ResPairFrag& w) { dh = res_mma(w.a, w.b, dh); }, [](auto) {});
+            pg = g;
+            pu = up;
+            pd = dh;
+        });
     fb_wait<0>();   // no copy is in flight when the block ends
 #pragma unroll
     for (int e = 0; e < 16; ++e) epi(e);
 #pragma unroll
-    for (int k = 0; k < 3; ++k) put(k, chunks - 1, false);
+    for (int k = 0; k < 3; ++k) put(k, chunks - 1);
 }
 
 // Y (n x co) of 128 rows.  KT: 16-element steps of the wider of ci and co (4, 8 or 16).  The hidden rows of a chunk pass
