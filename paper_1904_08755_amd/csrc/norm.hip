@@ -4,8 +4,13 @@
 //   g = dy gamma,  dx = r (g - mean(g) - h mean(g h)),  dgamma = sum over rows of dy h,  dbeta = sum of dy
 //
 // All sums are held in float32 (the sums over rows end in float64), in a fixed order: results are
-// bit-reproducible.  The mean is taken of x - x[0], so a row whose values share a large offset
-// loses no digits of its variance.
+// bit-reproducible.
+//
+// The mean is taken in two steps: m1 = x[0] + mean(x - x[0]) rounded to float32, then, with e = x - m1, its rest m2 =
+// mean(e), a few roundings of m1's size.  x - m is e - m2 and v is mean(e^2) - m2^2, both sums in one round of
+// exchanges.  (The difference loses no digits: m2 is at most about half a step of float32 at m1, and rows that are not
+// constant have a deviation of that size at least.)  So neither an offset that a row's values share nor a first value far
+// larger than the others costs digits.
 //
 // Bound: HBM (a read and a write of n x c forward, two reads and a write backward).  A row stays
 // in the registers of LPR lanes (NV pieces of 16 bytes a lane), so it is read once; a wave holds
@@ -122,30 +127,31 @@ __global__ void __launch_bounds__(kLnThreads) k_ln_fwd(const T* X, int64_t n, in
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const bool in = ln_whole<NV>(i) || (i * LPR + l) * V + (TAIL ? e : 0) < c;
-                v[i][e] = in ? R::get(raw[i], e) - x0 : 0.f;
-                s += v[i][e];
+                s += in ? R::get(raw[i], e) - x0 : 0.f;
             }
-        const float m = row_sum<LPR>(s) * inv_c;
-        float q = 0.f;
+        const float m1 = x0 + row_sum<LPR>(s) * inv_c;
+        float t = 0.f, q = 0.f;
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const bool in = ln_whole<NV>(i) || (i * LPR + l) * V + (TAIL ? e : 0) < c;
-                v[i][e] = in ? v[i][e] - m : 0.f;
+                v[i][e] = in ? R::get(raw[i], e) - m1 : 0.f;
+                t += v[i][e];
                 q = fmaf(v[i][e], v[i][e], q);
             }
-        const float r = 1.f / sqrtf(row_sum<LPR>(q) * inv_c + eps);
+        const float m2 = row_sum<LPR>(t) * inv_c;
+        const float r = 1.f / sqrtf(fmaf(-m2, m2, row_sum<LPR>(q) * inv_c) + eps);
 #pragma unroll
         for (int i = 0; i < NV; ++i) {
             const int col = (i * LPR + l) * V;
             float o[V];
 #pragma unroll
-            for (int e = 0; e < V; ++e) o[e] = fmaf(v[i][e] * r, ga[i][e], be[i][e]);
+            for (int e = 0; e < V; ++e) o[e] = fmaf((v[i][e] - m2) * r, ga[i][e], be[i][e]);
             store_piece<T, NV, TAIL>(Y + row * c, i, col, c, o);
         }
         if (l == 0) {
-            if (mean) mean[row] = x0 + m;
+            if (mean) mean[row] = m1 + m2;
             if (rstd) rstd[row] = r;
         }
     }
@@ -171,19 +177,21 @@ __global__ void __launch_bounds__(kLnThreads) k_ln_fwd_wide(const T* X, int64_t 
     for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
         const T* x = X + row * c;
         const float x0 = to_f32(x[0]);
-        float s = 0.f, q = 0.f;
+        float s = 0.f, t = 0.f, q = 0.f;
         for (int i = threadIdx.x; i < c; i += kLnThreads) s += to_f32(x[i]) - x0;
-        const float m = ln_block_sum(s, sh) / (float)c;
+        const float m1 = x0 + ln_block_sum(s, sh) / (float)c;
         for (int i = threadIdx.x; i < c; i += kLnThreads) {
-            const float d = to_f32(x[i]) - x0 - m;
-            q = fmaf(d, d, q);
+            const float e = to_f32(x[i]) - m1;
+            t += e;
+            q = fmaf(e, e, q);
         }
-        const float r = 1.f / sqrtf(ln_block_sum(q, sh) / (float)c + eps);   // (also: every thread has read x[0])
+        const float m2 = ln_block_sum(t, sh) / (float)c;
+        const float r = 1.f / sqrtf(fmaf(-m2, m2, ln_block_sum(q, sh) / (float)c) + eps);   // (every thread has read x[0])
         for (int i = threadIdx.x; i < c; i += kLnThreads)
             store_out(&Y[row * c + i],
-                      fmaf((to_f32(x[i]) - x0 - m) * r, gamma ? gamma[i] : 1.f, beta ? beta[i] : 0.f));
+                      fmaf((to_f32(x[i]) - m1 - m2) * r, gamma ? gamma[i] : 1.f, beta ? beta[i] : 0.f));
         if (threadIdx.x == 0) {
-            if (mean) mean[row] = x0 + m;
+            if (mean) mean[row] = m1 + m2;
             if (rstd) rstd[row] = r;
         }
     }

@@ -780,3 +780,52 @@ def test_transformer_block_on_a_sparse_tensor():
         err = float((o.detach().double().view(r.shape) - r.detach()).abs().max() / r.detach().abs().max())
         print(name, err)
         assert err <= tol, (name, err)
+
+
+# --------------------------------------------------------------------------- #
+# digits
+# --------------------------------------------------------------------------- #
+def _ln_digits(x, eps):
+    """(d, rstd, mean) of float64 rows and the bounds of what float32 makes of them, k roundings a sum of a row: m1, the
+    first step of the mean, is off by at most m2 (k roundings of |x - x0| and its own), and then counts by its roundings
+    alone: e = x - m1 has one, its sums k, x - m = e - mean(e) one more, v = mean(e^2) - mean(e)^2 the sums'."""
+    k = max(32, x.shape[1] // 256) + 11
+    m = x.mean(1, keepdim=True)
+    d = x - m
+    v = d.square().mean(1, keepdim=True)
+    r = (v + eps).rsqrt()
+    m2 = k * U * (x - x[:, :1]).abs().mean(1, keepdim=True) + 2 * U * m.abs()
+    mad = d.abs().mean(1, keepdim=True) + m2
+    e_m = (k + 1) * U * mad
+    e_d = U * (2 * d.abs() + m2) + e_m
+    e_v = (k + 4) * U * (v + m2 * m2) + 2 * m2 * e_m
+    e_r = r * (e_v / (2 * (v + eps)) + 4 * U)
+    return (d, r, m), (e_d, e_r, e_m + U * (m.abs() + m2))
+
+
+def _rows_with_one_large(g, n, c, big, where, dtype):
+    """Rows of size 1 whose value at `where` is `big` times as large."""
+    X = torch.randn((n, c), generator=g, device=DEV)
+    X[:, where] = big * (1 + 0.1 * torch.rand(n, generator=g, device=DEV))
+    return X.to(dtype)
+
+
+LN_DIGITS = [24, 96, 257, 1027, 2048, 3000]
+
+
+@BOTH
+@pytest.mark.parametrize("c", LN_DIGITS)
+@pytest.mark.parametrize("big", [1e2, 1e4, 1e6])
+def test_layer_norm_one_large_value(dtype, c, big):
+    """One channel far larger than the others, first, in the middle and last: the others keep their digits."""
+    g = _gen(c, big)
+    ga, be = 1 + 0.3 * torch.randn(c, generator=g, device=DEV), 0.3 * torch.randn(c, generator=g, device=DEV)
+    for where in (0, 5, c - 1):
+        X = _rows_with_one_large(g, 200, c, big, where, dtype)
+        (d, r, m), (e_d, e_r, e_m) = _ln_digits(X.double(), 1e-5)
+        Y, mean, rstd = gsc.gsc_layer_norm_fwd(X, ga, be, 1e-5)
+        _close(mean, m[:, 0], e_m[:, 0] * 1.01, ("mean", where))
+        _close(rstd, r[:, 0], e_r[:, 0] * 1.01, ("rstd", where))
+        y = d * r * ga.double() + be.double()
+        e = (d.abs() * e_r + e_d * r + 2 * U * (d * r).abs()) * ga.double().abs() + (2 * U + HALF[dtype]) * y.abs()
+        _close(Y, y, e * 1.01, ("Y", where))
