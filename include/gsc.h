@@ -577,8 +577,10 @@ int gsc_layer_norm_fwd(int32_t dtype, const void* X, int64_t n, int32_t c, const
 /* Gradients of gsc_layer_norm_fwd.  With h = (x - m) r and g = dy gamma:
  *   dX = r (g - mean(g) - h mean(g h))   (n x c of dtype; may be X or dY itself),
  *   dgamma = sum over rows of dy h,  dbeta = sum over rows of dy   (c float32),
- * each nullable.  mean, rstd: as the forward pass wrote them.  With n = 0 the
- * sums are 0.  ws: gsc_layer_norm_bwd_ws_bytes(n, c) bytes, needed only for
+ * each nullable.  mean, rstd: as the forward pass wrote them (what the mean's
+ * rounding leaves of x - m is taken out of the row again, so that an offset which
+ * the row's values share costs no digits here either).  With n = 0 the sums are
+ * 0.  ws: gsc_layer_norm_bwd_ws_bytes(n, c) bytes, needed only for
  * the sums, aligned to 4 bytes.  Asynchronous.  Errors: EINVAL, ESHORT (ws),
  * EHIP. */
 size_t gsc_layer_norm_bwd_ws_bytes(int64_t n, int32_t c);

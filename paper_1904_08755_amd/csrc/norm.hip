@@ -10,7 +10,8 @@
 // mean(e), a few roundings of m1's size.  x - m is e - m2 and v is mean(e^2) - m2^2, both sums in one round of
 // exchanges.  (The difference loses no digits: m2 is at most about half a step of float32 at m1, and rows that are not
 // constant have a deviation of that size at least.)  So neither an offset that a row's values share nor a first value far
-// larger than the others costs digits.
+// larger than the others costs digits.  The backward pass gets m1 + m2 rounded to float32, and where a row's values share an
+// offset that rounding is as large as their deviations: it takes x - mean, and out of that the rest's mean, again.
 //
 // Bound: HBM (a read and a write of n x c forward, two reads and a write backward).  A row stays
 // in the registers of LPR lanes (NV pieces of 16 bytes a lane), so it is read once; a wave holds
@@ -18,7 +19,8 @@
 // their columns' gamma, beta and (backward) column sums in registers over all rows they visit.
 // Measured: 300,000 rows of 256 bfloat16 columns forward 55 us (5.6 TB/s), backward 92 us and 5 us for the sums (5.0 TB/s);
 // 20,011 rows of 1,027 (rows at odd addresses, a third of the lanes idle in the last piece) 20 and 36 us (4.2 and 3.5 TB/s).
-// Rows of more than kLnRegCols columns take a block each and are read again for each sum (from the L2).
+// Rows of more than kLnRegCols columns take a block each and are read again for each sum (from the L2); with the sums over
+// rows the backward pass is a block a row for the rows' means, and then a thread a column for dX and the sums.
 #include "row_vec.h"
 
 namespace gsc {
@@ -197,6 +199,11 @@ __global__ void __launch_bounds__(kLnThreads) k_ln_fwd_wide(const T* X, int64_t 
     }
 }
 
+// An element of dX (the same operations wherever it is formed), a = mean(g), b = mean(g h).
+__device__ __forceinline__ float ln_dx(float dy, float ga, float h, float r, float a, float b) {
+    return r * fmaf(-h, b, fmaf(dy, ga, -a));
+}
+
 // part: per block, the c column sums of dy h, then of dy.
 template <typename T, int LPR, int NV, bool TAIL>
 __global__ void __launch_bounds__(kLnThreads) k_ln_bwd(const T* X, const T* dY, int64_t n, int c,
@@ -220,33 +227,33 @@ __global__ void __launch_bounds__(kLnThreads) k_ln_bwd(const T* X, const T* dY, 
         load_row<T, LPR, NV, TAIL>(X + row * c, l, c, xr);
         load_row<T, LPR, NV, TAIL>(dY + row * c, l, c, yr);
         const float m = mean[row], r = rstd[row];
-        float a = 0.f, b = 0.f;   // sums of g and of g h
+        float t = 0.f, a = 0.f, b = 0.f;   // sums of x - m, of g and of g (x - m)
 #pragma unroll
         for (int i = 0; i < NV; ++i)
 #pragma unroll
             for (int e = 0; e < V; ++e) {
                 const bool in = ln_whole<NV>(i) || (i * LPR + l) * V + (TAIL ? e : 0) < c;
-                const float h = in ? (R::get(xr[i], e) - m) * r : 0.f;
-                const float d = R::get(yr[i], e), g = d * ga[i][e];
-                sg[i][e] = fmaf(d, h, sg[i][e]);
-                sb[i][e] += d;
+                const float d = in ? R::get(xr[i], e) - m : 0.f;
+                const float g = R::get(yr[i], e) * ga[i][e];
+                t += d;
                 a += g;
-                b = fmaf(g, h, b);
+                b = fmaf(g, d, b);
             }
-        if (dX) {
-            a = row_sum<LPR>(a) * inv_c;
-            b = row_sum<LPR>(b) * inv_c;
+        const float m2 = row_sum<LPR>(t) * inv_c;
+        a = row_sum<LPR>(a) * inv_c;
+        b = fmaf(-m2, a, row_sum<LPR>(b) * inv_c) * r;   // mean of g h
 #pragma unroll
-            for (int i = 0; i < NV; ++i) {
-                const int col = (i * LPR + l) * V;
-                float o[V];
+        for (int i = 0; i < NV; ++i) {
+            const int col = (i * LPR + l) * V;
+            float o[V];
 #pragma unroll
-                for (int e = 0; e < V; ++e) {
-                    const float h = (R::get(xr[i], e) - m) * r;
-                    o[e] = r * (R::get(yr[i], e) * ga[i][e] - a - h * b);
-                }
-                store_piece<T, NV, TAIL>(dX + row * c, i, col, c, o);
+            for (int e = 0; e < V; ++e) {
+                const float h = (R::get(xr[i], e) - m - m2) * r, d = R::get(yr[i], e);
+                sg[i][e] = fmaf(d, h, sg[i][e]);   // (behind the row's end dy is 0, and no column is stored)
+                sb[i][e] += d;
+                o[e] = ln_dx(d, ga[i][e], h, r, a, b);
             }
+            if (dX) store_piece<T, NV, TAIL>(dX + row * c, i, col, c, o);
         }
     }
     if (!part) return;
@@ -273,47 +280,73 @@ __global__ void __launch_bounds__(kLnThreads) k_ln_bwd(const T* X, const T* dY, 
     }
 }
 
+// dX, or, with `rows`, what it (or, where it is null, what the sums over rows) takes of each row: m2, mean(g) and mean(g h).
 template <typename T>
 __global__ void __launch_bounds__(kLnThreads) k_ln_bwd_wide(const T* X, const T* dY, int64_t n, int c,
                                                             const float* __restrict__ gamma,
                                                             const float* __restrict__ mean,
-                                                            const float* __restrict__ rstd, T* dX) {
+                                                            const float* __restrict__ rstd, T* dX,
+                                                            float* __restrict__ rows) {
     __shared__ float sh[kLnThreads / 64];
     for (int64_t row = blockIdx.x; row < n; row += gridDim.x) {
         const T* x = X + row * c;
         const T* dy = dY + row * c;
         const float m = mean[row], r = rstd[row];
-        float a = 0.f, b = 0.f;
-        for (int i = threadIdx.x; i < c; i += kLnThreads) {
-            const float g = to_f32(dy[i]) * (gamma ? gamma[i] : 1.f);
-            a += g;
-            b = fmaf(g, (to_f32(x[i]) - m) * r, b);
+        float t = 0.f, a = 0.f, b = 0.f;
+        if (!dX) {
+            for (int i = threadIdx.x; i < c; i += kLnThreads) t += to_f32(x[i]) - m;
+            t = ln_block_sum(t, sh) / (float)c;
+            if (threadIdx.x == 0) rows[3 * row] = t;
+            continue;
         }
-        a = ln_block_sum(a, sh) / (float)c;
-        b = ln_block_sum(b, sh) / (float)c;
         for (int i = threadIdx.x; i < c; i += kLnThreads) {
-            const float g = to_f32(dy[i]) * (gamma ? gamma[i] : 1.f), h = (to_f32(x[i]) - m) * r;
-            store_out(&dX[row * c + i], r * (g - a - h * b));
+            const float g = to_f32(dy[i]) * (gamma ? gamma[i] : 1.f), d = to_f32(x[i]) - m;
+            t += d;
+            a += g;
+            b = fmaf(g, d, b);
+        }
+        const float m2 = ln_block_sum(t, sh) / (float)c;
+        a = ln_block_sum(a, sh) / (float)c;
+        b = fmaf(-m2, a, ln_block_sum(b, sh) / (float)c) * r;
+        if (rows) {
+            if (threadIdx.x == 0) rows[3 * row] = m2, rows[3 * row + 1] = a, rows[3 * row + 2] = b;
+            continue;
+        }
+        for (int i = threadIdx.x; i < c; i += kLnThreads) {
+            const float h = (to_f32(x[i]) - m - m2) * r;
+            store_out(&dX[row * c + i], ln_dx(to_f32(dy[i]), gamma ? gamma[i] : 1.f, h, r, a, b));
         }
     }
 }
 
-// Column sums of wide rows: a thread takes a column of a chunk's rows.
+// Column sums of wide rows and, unless null, dX: a thread takes a column of a chunk's rows.
 template <typename T>
-__global__ void __launch_bounds__(kLnThreads) k_ln_bwd_wide_cols(const T* __restrict__ X, const T* __restrict__ dY,
-                                                                 int64_t n, int c, const float* __restrict__ mean,
+__global__ void __launch_bounds__(kLnThreads) k_ln_bwd_wide_cols(const T* X, const T* dY, int64_t n, int c,
+                                                                 const float* __restrict__ gamma,
+                                                                 const float* __restrict__ mean,
                                                                  const float* __restrict__ rstd,
+                                                                 const float* __restrict__ rows, T* dX,
                                                                  float* __restrict__ part) {
     const int64_t chunks = gridDim.x, k = blockIdx.x;
     const int64_t r0 = n * k / chunks, r1 = n * (k + 1) / chunks;
     for (int col = blockIdx.y * kLnThreads + threadIdx.x; col < c; col += gridDim.y * kLnThreads) {
         float sg = 0.f, sb = 0.f;
-#pragma unroll 4
-        for (int64_t row = r0; row < r1; ++row) {
-            const float d = to_f32(dY[row * c + col]);
-            sg = fmaf(d, (to_f32(X[row * c + col]) - mean[row]) * rstd[row], sg);
+        const float ga = gamma ? gamma[col] : 1.f;
+        auto add = [&](int64_t row, T x, T dy) {
+            const float r = rstd[row], d = to_f32(dy), h = (to_f32(x) - mean[row] - rows[3 * row]) * r;
+            sg = fmaf(d, h, sg);
             sb += d;
+            if (dX) store_out(&dX[row * c + col], ln_dx(d, ga, h, r, rows[3 * row + 1], rows[3 * row + 2]));
+        };
+        int64_t row = r0;
+        for (; row + 4 <= r1; row += 4) {   // (four rows are read before the first is written: dX may be X or dY)
+            T x[4], dy[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) x[i] = X[(row + i) * c + col], dy[i] = dY[(row + i) * c + col];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) add(row + i, x[i], dy[i]);
         }
+        for (; row < r1; ++row) add(row, X[row * c + col], dY[row * c + col]);
         part[k * 2 * c + col] = sg;
         part[(k * 2 + 1) * c + col] = sb;
     }
@@ -398,6 +431,9 @@ static void ln_fwd(const void* X_, int64_t n, int c, const float* gamma, const f
     });
 }
 
+// Floats of the workspace: the chunks' column sums, then (wide rows) three of each row.
+static size_t ln_part(int64_t n, int c) { return (size_t)ln_row_blocks(n, kLnThreads / 64, kLnChunks) * 2 * (size_t)c; }
+
 // Launches the passes over the rows; returns the number of chunks whose sums are in part.
 template <typename T>
 static int64_t ln_bwd(const void* X_, const void* dY_, int64_t n, int c, const float* gamma, const float* mean,
@@ -407,14 +443,18 @@ static int64_t ln_bwd(const void* X_, const void* dY_, int64_t n, int c, const f
     T* dX = reinterpret_cast<T*>(dX_);
     int64_t chunks = 0;
     if (c > kLnRegCols) {
-        chunks = ln_row_blocks(n, 64, kLnChunks);
+        // of 64 rows, or of fewer, down to 8, while there are under 1,024 blocks (300 rows of 8,192 bfloat16 columns: 23 us, 29)
         const unsigned cb = (unsigned)((c + kLnThreads - 1) / kLnThreads);
-        if (part)   // before dX is written, which may be dY itself
-            hipLaunchKernelGGL(k_ln_bwd_wide_cols<T>, dim3((unsigned)chunks, cb < 4096 ? cb : 4096), dim3(kLnThreads),
-                               0, s, X, dY, n, c, mean, rstd, part);
-        if (dX && n > 0)
+        const int64_t most = ln_row_blocks(n, 8, 1024 / cb + 1);
+        chunks = ln_row_blocks(n, 64, kLnChunks);
+        if (chunks < most) chunks = most;
+        float* rows = part ? part + ln_part(n, c) : nullptr;
+        if (n > 0)
             hipLaunchKernelGGL(k_ln_bwd_wide<T>, dim3((unsigned)ln_row_blocks(n, 1, kLnFwdBlocks)), dim3(kLnThreads),
-                               0, s, X, dY, n, c, gamma, mean, rstd, dX);
+                               0, s, X, dY, n, c, gamma, mean, rstd, dX, rows);
+        if (part)
+            hipLaunchKernelGGL(k_ln_bwd_wide_cols<T>, dim3((unsigned)chunks, cb < 4096 ? cb : 4096), dim3(kLnThreads),
+                               0, s, X, dY, n, c, gamma, mean, rstd, rows, dX, part);
         return chunks;
     }
     ln_dispatch<T, 3>(c, [&](auto LPR, auto NV, auto TAIL) {
@@ -451,7 +491,7 @@ int gsc_layer_norm_fwd(int32_t dtype, const void* X, int64_t n, int32_t c, const
 
 size_t gsc_layer_norm_bwd_ws_bytes(int64_t n, int32_t c) {
     if (n < 0 || c < 1 || c > kLnMaxCols) return 0;
-    return (size_t)ln_row_blocks(n, kLnThreads / 64, kLnChunks) * 2 * (size_t)c * sizeof(float);
+    return (ln_part(n, c) + (c > kLnRegCols ? 3 * (size_t)n : 0)) * sizeof(float);
 }
 
 int gsc_layer_norm_bwd(int32_t dtype, const void* X, const void* dY, int64_t n, int32_t c, const float* gamma,

@@ -829,3 +829,50 @@ def test_layer_norm_one_large_value(dtype, c, big):
         y = d * r * ga.double() + be.double()
         e = (d.abs() * e_r + e_d * r + 2 * U * (d * r).abs()) * ga.double().abs() + (2 * U + HALF[dtype]) * y.abs()
         _close(Y, y, e * 1.01, ("Y", where))
+
+
+def _ln_grads(x, dy, ga, eps):
+    """float64 gradients of rows and their bounds, from the rows alone (as _ln_digits; sums of k terms)."""
+    k = max(32, x.shape[1] // 256) + 12
+    (d, r, m), (e_d, e_r, _) = _ln_digits(x, eps)
+    h, gg = d * r, dy * ga
+    e_h = e_d * r + d.abs() * e_r + 3 * U * h.abs()
+    a, b = gg.mean(1, keepdim=True), (gg * h).mean(1, keepdim=True)
+    e_a = k * U * gg.abs().mean(1, keepdim=True)
+    # mean(g h) is (mean(g (x - m1)) - m2 mean(g)) r: the sums' roundings, h's errors, r's
+    m2 = 2 * U * m.abs() + k * U * d.abs().mean(1, keepdim=True)
+    e_b = (gg.abs() * e_h).mean(1, keepdim=True) + 3 * k * U * r * (gg.abs() * (d.abs() + m2)).mean(1, keepdim=True)
+    dx = r * (gg - a - h * b)
+    e_dx = r * (e_a + e_h * b.abs() + (h.abs() + e_h) * e_b + 6 * U * (gg.abs() + a.abs() + (h * b).abs())) + e_r * (dx / r).abs()
+    return (dx, (dy * h).sum(0), dy.sum(0)), (e_dx, (dy.abs() * (e_h + (108 + len(x) / 1024) * U * h.abs())).sum(0),
+                                              (108 + len(x) / 1024) * U * dy.abs().sum(0))
+
+
+@BOTH
+@pytest.mark.parametrize("c", LN_DIGITS)
+@pytest.mark.parametrize("rows", ["offset", "far offset", "large first", "large last"])
+def test_layer_norm_backward_digits(dtype, c, rows):
+    """Rows whose values share an offset far larger than their deviations, and rows with one large value, against
+    float64 gradients of the rows (not of the statistics that the forward pass gave)."""
+    g = _gen(c, len(rows))
+    n = 300
+    if "offset" in rows:
+        off, sd = (1e4, 1e-2) if rows == "offset" else (3e6, 1.0)
+        if dtype == torch.bfloat16:   # (its steps at 10,000 are 64)
+            sd = off / 300
+        X = (off * (1 + torch.rand((n, 1), generator=g, device=DEV)) + sd * torch.randn((n, c), generator=g, device=DEV)).to(dtype)
+    else:
+        X = _rows_with_one_large(g, n, c, 1e4, 0 if rows == "large first" else c - 1, dtype)
+    dY = _randn(g, n, c, dtype=dtype)
+    ga = 1 + 0.3 * torch.randn(c, generator=g, device=DEV)
+    eps = 1e-12
+    _, mean, rstd = gsc.gsc_layer_norm_fwd(X, ga, None, eps)
+    refs, bounds = _ln_grads(X.double(), dY.double(), ga.double(), eps)
+    got = gsc.gsc_layer_norm_bwd(X, dY, mean, rstd, ga)
+    _close(got[0], refs[0], bounds[0] * 1.01 + HALF[dtype] * refs[0].abs() * 1.01, "dX")
+    _close(got[1], refs[1], bounds[1] * 1.01 + U * refs[1].abs(), "dgamma")
+    _close(got[2], refs[2], bounds[2] * 1.01 + U * refs[2].abs(), "dbeta")
+    assert torch.equal(gsc.gsc_layer_norm_bwd(X, dY, mean, rstd, ga, need_sums=False)[0], got[0])
+    assert torch.equal(gsc.gsc_layer_norm_bwd(X, dY, mean, rstd, ga, need_dx=False)[1], got[1])
+    out = gsc.gsc_layer_norm_bwd(X, dY, mean, rstd, ga, dX=dY)   # in place
+    assert torch.equal(out[0], got[0]) and torch.equal(out[1], got[1])

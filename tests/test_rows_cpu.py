@@ -111,3 +111,10 @@ def test_binding_refuses_host_tensors():
         gsc.gsc_gated_ffn_fwd(x, torch.zeros(8, 4), torch.zeros(8, 4), torch.zeros(4, 8))
     with pytest.raises(ValueError, match="dtype"):
         gsc.gsc_layer_norm_fwd(x.half())
+
+
+def test_layer_norm_wide_workspace(L):
+    """Rows of over 2,048 columns: the chunks' column sums and three floats of each row."""
+    assert L.gsc_layer_norm_bwd_ws_bytes(7, 2048) == 2 * 2 * 2048 * 4
+    assert L.gsc_layer_norm_bwd_ws_bytes(7, 2049) == 2 * 2 * 2049 * 4 + 3 * 7 * 4
+    assert L.gsc_layer_norm_bwd_ws_bytes(10**7, 4096) == 1024 * 2 * 4096 * 4 + 3 * 10**7 * 4
