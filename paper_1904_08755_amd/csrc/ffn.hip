@@ -111,7 +111,7 @@ __device__ __forceinline__ void store_hidden(const floatx4 (&acc)[MT][4], int64_
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float a, d;
-                    ffn_act<decltype(ACT)::value, false>(acc[mi][ni][e], a, d);
+                    ffn_act<decltype(ACT)::value, false, sizeof(T) == 2>(acc[mi][ni][e], a, d);
                     h[ni][e] = a * acc[mi][ni + 2][e];
                 }
             store_pair(H.at(row, col0).p, 4 * ffn_q(), 32, row < n, h[0], h[1]);
@@ -134,7 +134,7 @@ __device__ __forceinline__ void store_mid(const floatx4 (&acc)[MT][4], const flo
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     float a, d;
-                    ffn_act<decltype(ACT)::value, true>(acc[mi][ni][e], a, d);
+                    ffn_act<decltype(ACT)::value, true, sizeof(T) == 2>(acc[mi][ni][e], a, d);
                     const float up = acc[mi][ni + 2][e], g = dh[mi][ni][e];
                     h[ni][e] = a * up;
                     dg[ni][e] = g * up * d;
@@ -575,7 +575,7 @@ k_ffn_few(const TA* __restrict__ A, int64_t lda, int n, int k, const T* __restri
         if (GATED)
             with_act(act, [&](auto ACT) {
                 float a, d;
-                ffn_act<decltype(ACT)::value, false>(v[0], a, d);
+                ffn_act<decltype(ACT)::value, false, sizeof(T) == 2>(v[0], a, d);
                 o = a * v[NB - 1];
             });
         store_out(&out[r * ldo + c], o);

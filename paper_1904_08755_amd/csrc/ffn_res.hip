@@ -197,7 +197,7 @@ k_ffn_mid_res(const uint16_t* __restrict__ X, const uint16_t* __restrict__ dY, i
     uint32_t ph[8];
     auto epi = [&](int e) {
         float a, d;
-        ffn_act<ACT, true>(pg[e], a, d);
+        ffn_act<ACT, true, true>(pg[e], a, d);
         const float up = pu[e], g = pd[e];
         pd[e] = a * up;
         pg[e] = g * up * d;
@@ -287,7 +287,7 @@ k_ffn_fwd_res(const uint16_t* __restrict__ X, int64_t n, int ci, int co, const u
     float v[4];
     auto epi = [&](int e) {
         float a, d;
-        ffn_act<ACT, false>(pg[e], a, d);
+        ffn_act<ACT, false, true>(pg[e], a, d);
         v[e & 3] = a * pu[e];
         if ((e & 3) == 3)   // columns 32 wn + 8 j + 4 h .., j = e / 4: half of piece 4 wn + j
             *reinterpret_cast<uint2*>(hid + row * 128 + (((4 * wn + (e >> 2)) ^ (row & 7)) * 16) + h * 8) =

@@ -176,7 +176,7 @@ k_ffn_fwd_rows(const float* __restrict__ X, int64_t n, int ci, const float* __re
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             float a, d;
-            ffn_act<ACT, false>(g[e], a, d);
+            ffn_act<ACT, false, false>(g[e], a, d);
             g[e] = a * u[e];
         }
         __builtin_amdgcn_sched_barrier(0);   // (the next chunk's registers live while u's do not)
@@ -228,7 +228,7 @@ k_ffn_bwd_rows(const float* __restrict__ X, const float* __restrict__ dY, int64_
 #pragma unroll
         for (int e = 0; e < 16; ++e) {
             float a, s;
-            ffn_act<ACT, true>(g[e], a, s);
+            ffn_act<ACT, true, false>(g[e], a, s);
             g[e] = d[e] * u[e] * s;
             u[e] = a * u[e];
             d[e] = d[e] * a;

@@ -876,3 +876,56 @@ def test_layer_norm_backward_digits(dtype, c, rows):
     assert torch.equal(gsc.gsc_layer_norm_bwd(X, dY, mean, rstd, ga, need_dx=False)[1], got[1])
     out = gsc.gsc_layer_norm_bwd(X, dY, mean, rstd, ga, dX=dY)   # in place
     assert torch.equal(out[0], got[0]) and torch.equal(out[1], got[1])
+
+
+def _act_digits(act, g):
+    """(act(g), its derivative) in float64 and their bounds in float32: units of 2^-24 of the value, and twice as many of
+    the sizes of the derivative's two terms.  What grows with g is the rounding of the exponential's argument x, one or two
+    units of |x| for the square or the cubic and half a one for log2(e); the hardware's exponential and reciprocal have
+    two units each, the polynomials' terms and the products a few."""
+    a, d = _act64(act, g)
+    if act == "relu":
+        return (a, d), (a * 0, d * 0)
+    if act == "gelu":
+        units = 1.25 * g * g + 16
+        a = g * 0.5 * torch.erfc(-g * math.sqrt(0.5))
+        terms = (a / g).abs() + g.abs() * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+        d = a / g + g * torch.exp(-g * g / 2) / math.sqrt(2 * math.pi)
+    else:
+        x, dx = g, torch.ones_like(g)
+        if act == "gelu_tanh":
+            k = 2 * math.sqrt(2 / math.pi)
+            x, dx = k * (g + 0.044715 * g ** 3), k * (1 + 3 * 0.044715 * g * g)
+        units = 6 * x.abs() + 10 if act == "gelu_tanh" else 1.5 * x.abs() + 8
+        p, q = torch.sigmoid(x), torch.sigmoid(-x)
+        a = p if act == "sigmoid" else g * p
+        d = p * q if act == "sigmoid" else p + g * p * q * dx
+        terms = d.abs() if act == "sigmoid" else p + (g * p * q * dx).abs()
+    return (a, d), (units * U * a.abs(), 2 * units * U * terms)
+
+
+ACT_ROWS = [  # dtype, rows, c_in: a few rows, tiles, rows in registers forward and backward
+    (torch.float32, 4, 2), (torch.float32, 200, 2), (torch.float32, 200, 40), (torch.float32, 32768, 2),
+    (torch.float32, 32768, 40), (torch.bfloat16, 4, 2), (torch.bfloat16, 200, 2), (torch.bfloat16, 12800, 2),
+    (torch.bfloat16, 700_000, 66)]
+
+
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("dtype,n,ci", ACT_ROWS)
+def test_gated_ffn_activation_digits(act, dtype, n, ci):
+    """act(g) and its derivative relative to their own sizes, for gates from -6 to 6: the gate is the first channel, its
+    partner the second, which is 1, and the last product is with 1."""
+    W = torch.zeros((2, ci, 1), dtype=dtype, device=DEV)
+    W[0, 0] = W[1, 1] = 1
+    Wd = torch.ones((1, 1), dtype=dtype, device=DEV)
+    for g in torch.linspace(-6, 6, max(n, 64), device=DEV).to(dtype).split(n):
+        X = torch.zeros((len(g), ci), dtype=dtype, device=DEV)
+        X[:, 0], X[:, 1] = g, 1
+        (a, d), (e_a, e_d) = _act_digits(act, g.double())
+        Y = gsc.gsc_gated_ffn_fwd(X, W[0], W[1], Wd, act)
+        dX = gsc.gsc_gated_ffn_bwd(X, W[0], W[1], Wd, torch.ones_like(Y), act, need_dw=False)[0]
+        # bfloat16: the hidden row's rounding, or dG's and dU's, and the result's
+        low = 0.0 if dtype == torch.float32 else 2 * HALF[dtype] * 1.01
+        _close(Y[:, 0], a, e_a + low * a.abs(), act)
+        _close(dX[:, 0], d, e_d + low * d.abs(), (act, "derivative"))
+        _close(dX[:, 1], a, e_a + low * a.abs(), (act, "partner"))
