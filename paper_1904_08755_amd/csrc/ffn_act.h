@@ -75,9 +75,10 @@ __device__ __forceinline__ void ffn_act(float g, float& a, float& d) {
         a = g * p;
         if (D) d = fmaf(g * 0.398942280401433f, e, p);
     } else {
-        // 0.5 (1 + tanh(u / 2)) = sigmoid(u).
+        // 0.5 (1 + tanh(u / 2)) = sigmoid(u).  The square is held at 10^4, where the sigmoid is long 0 or 1: without it the
+        // derivative is 0 times infinity from |g| = 1.9e19 on.
         const float k = 1.59576912160573f, c = 0.044715f;   // 2 sqrt(2 / pi)
-        const float g2 = g * g;
+        const float g2 = fminf(g * g, 1e4f);
         float p, q;
         ffn_sigmoid<D>(k * g * fmaf(c, g2, 1.f), p, q);
         a = g * p;

@@ -929,3 +929,19 @@ def test_gated_ffn_activation_digits(act, dtype, n, ci):
         _close(Y[:, 0], a, e_a + low * a.abs(), act)
         _close(dX[:, 0], d, e_d + low * d.abs(), (act, "derivative"))
         _close(dX[:, 1], a, e_a + low * a.abs(), (act, "partner"))
+
+
+@BOTH
+@pytest.mark.parametrize("act", ACTS)
+@pytest.mark.parametrize("n", [4, 100])
+def test_gated_ffn_huge_gates(dtype, act, n):
+    """Gates up to the type's end: the activation's and the derivative's limits, nothing undefined."""
+    g = torch.tensor([-3e38, -1e30, -2e19, -1e5, 1e5, 2e19, 1e30, 3e38], device=DEV).to(dtype).repeat(13)[:n]
+    X = torch.stack([g, torch.ones_like(g)], 1).contiguous()
+    W = torch.eye(2, dtype=dtype, device=DEV)
+    Wg, Wu, Wd = W[:, :1].contiguous(), W[:, 1:].contiguous(), torch.ones((1, 1), dtype=dtype, device=DEV)
+    Y = gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd, act)
+    dX = gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, torch.ones_like(Y), act, need_dw=False)[0]
+    up = (g > 0).to(dtype)
+    a, d = (up, 0 * up) if act == "sigmoid" else (torch.where(g > 0, g, 0 * up), up)
+    assert torch.equal(Y[:, 0], a) and torch.equal(dX[:, 1], a) and torch.equal(dX[:, 0], d), (Y, dX)
