@@ -35,6 +35,7 @@ constexpr int64_t kLnChunks = 1024;     // row chunks (blocks) of the backward p
 // rows of 100 columns 70 and 45; float32, 79,922 rows of 257 columns in 12 elements a lane 51 and 44).
 static int64_t ln_most(int c, int per_lane, int64_t most) { return c > 256 && per_lane >= 16 ? most / 2 : most; }
 constexpr int kLnSumCh = 16, kLnSumLanes = 64;
+constexpr int64_t kLnSumBlocks = 65536;   // (a launch takes fewer than 2^32 threads: 2^22 blocks of these)
 
 static int64_t ln_row_blocks(int64_t n, int rows, int64_t most) {
     const int64_t b = (n + rows - 1) / rows;
@@ -359,22 +360,26 @@ k_ln_bwd_sum(const float* __restrict__ part, int64_t chunks, int c, float* __res
              float* __restrict__ dbeta) {
     __shared__ double sh[kLnSumLanes][kLnSumCh];
     const int ci = threadIdx.x % kLnSumCh, l = threadIdx.x / kLnSumCh;
-    const int64_t ch = (int64_t)blockIdx.x * kLnSumCh + ci, c2 = 2 * (int64_t)c;
-    double a = 0.0;
-    if (ch < c2) {
+    const int64_t c2 = 2 * (int64_t)c;
+    for (int64_t ch0 = (int64_t)blockIdx.x * kLnSumCh; ch0 < c2; ch0 += (int64_t)gridDim.x * kLnSumCh) {
+        const int64_t ch = ch0 + ci;
+        double a = 0.0;
+        if (ch < c2) {
 #pragma unroll 4
-        for (int64_t k = l; k < chunks; k += kLnSumLanes) a += part[k * c2 + ch];
-    }
-    sh[l][ci] = a;
-    for (int d = kLnSumLanes / 2; d > 0; d >>= 1) {
-        __syncthreads();
-        if (l < d) sh[l][ci] += sh[l + d][ci];
-    }
-    if (l == 0 && ch < c2) {
-        if (ch < c) {
-            if (dgamma) dgamma[ch] = (float)sh[0][ci];
-        } else if (dbeta) {
-            dbeta[ch - c] = (float)sh[0][ci];
+            for (int64_t k = l; k < chunks; k += kLnSumLanes) a += part[k * c2 + ch];
+        }
+        __syncthreads();   // the previous columns' sums are read
+        sh[l][ci] = a;
+        for (int d = kLnSumLanes / 2; d > 0; d >>= 1) {
+            __syncthreads();
+            if (l < d) sh[l][ci] += sh[l + d][ci];
+        }
+        if (l == 0 && ch < c2) {
+            if (ch < c) {
+                if (dgamma) dgamma[ch] = (float)sh[0][ci];
+            } else if (dbeta) {
+                dbeta[ch - c] = (float)sh[0][ci];
+            }
         }
     }
 }
@@ -516,7 +521,7 @@ int gsc_layer_norm_bwd(int32_t dtype, const void* X, const void* dY, int64_t n, 
                                              : ln_bwd<float>(X, dY, n, c, gamma, mean, rstd, dX, part, s);
     GSC_LAUNCH_CHECK();
     if (sums) {
-        hipLaunchKernelGGL(k_ln_bwd_sum, dim3((unsigned)((2 * (int64_t)c + kLnSumCh - 1) / kLnSumCh)),
+        hipLaunchKernelGGL(k_ln_bwd_sum, dim3((unsigned)ln_row_blocks(2 * (int64_t)c, kLnSumCh, kLnSumBlocks)),
                            dim3(kLnSumCh * kLnSumLanes), 0, s, part, chunks, c, dgamma, dbeta);
         GSC_LAUNCH_CHECK();
     }

@@ -945,3 +945,17 @@ def test_gated_ffn_huge_gates(dtype, act, n):
     up = (g > 0).to(dtype)
     a, d = (up, 0 * up) if act == "sigmoid" else (torch.where(g > 0, g, 0 * up), up)
     assert torch.equal(Y[:, 0], a) and torch.equal(dX[:, 1], a) and torch.equal(dX[:, 0], d), (Y, dX)
+
+
+def test_layer_norm_widest_rows():
+    """Rows of over 2^25 columns: the column sums' kernel walks over more columns than a launch has threads for."""
+    n, c = 2, (1 << 25) + 19
+    g = _gen(25)
+    X, dY = _randn(g, n, c, dtype=torch.bfloat16), _randn(g, n, c, dtype=torch.bfloat16)
+    _, mean, rstd = gsc.gsc_layer_norm_fwd(X)
+    dX, dgamma, dbeta = gsc.gsc_layer_norm_bwd(X, dY, mean, rstd)
+    x, dy = X.double(), dY.double()
+    refs, bounds = _ln_grads(x, dy, torch.ones(c, device=DEV, dtype=torch.float64), 1e-5)
+    _close(dX, refs[0], bounds[0] * 1.01 + HALF[torch.bfloat16] * refs[0].abs() * 1.01, "dX")
+    _close(dgamma, refs[1], bounds[1] * 1.01, "dgamma")
+    _close(dbeta, refs[2], bounds[2] * 1.01, "dbeta")
