@@ -642,6 +642,23 @@ static bool ffn_res_f32(const FfnShape& d, bool bwd) {
     return ffn_fills(d.n) || (!bwd && d.ci <= 32 && d.co <= 32);
 }
 
+// Which of the two ways a call of either type and pass goes.
+static bool ffn_res(int dtype, const FfnShape& d, bool bwd) {
+    if (dtype != GSC_BF16) return ffn_res_f32(d, bwd);
+    return bwd ? ffn_res_bwd(d) : ffn_res_fwd(d);
+}
+
+// Whether every launch of a call has fewer than 2^32 threads, the most that one takes.  Rows in registers: 512 (float32:
+// 256) threads for 128 rows.  Tiles: 256 for at least 128 rows (fewer only where few tiles are) by 64 columns.
+static bool ffn_launches(int dtype, const FfnShape& d, bool bwd) {
+    const int64_t tiles = ceil_div(d.n, 128);
+    int64_t widest = d.f > d.co ? d.f : d.co;
+    if (bwd && d.ci > widest) widest = d.ci;
+    const int64_t threads = !bwd && ffn_res(dtype, d, bwd) ? tiles * (dtype == GSC_BF16 ? 512 : 256)
+                                                           : tiles * ceil_div(widest, 64) * 256;
+    return threads < (int64_t)1 << 32;
+}
+
 // float32: tiles of 64 outputs instead of 128 in a direction where they leave less of the last one empty.
 static bool ffn_narrow(int64_t rows) { return ceil_div(rows, 64) % 2 == 1 && rows < 512; }
 
@@ -926,11 +943,10 @@ int gsc_gated_ffn_fwd(int32_t dtype, const void* X, int64_t n, int32_t c_in, con
     if (!ffn_sizes_ok(dtype, n, c_in, hidden, c_out))
         return fail(GSC_EINVAL, "gated_ffn_fwd: bad sizes n=%lld c_in=%d hidden=%d c_out=%d", (long long)n, c_in, hidden,
                     c_out);
-    if (ceil_div(n, 64) * ceil_div(hidden > c_out ? hidden : c_out, 64) > 0x7fffffff)
-        return fail(GSC_EINVAL, "gated_ffn_fwd: more tiles than a launch takes");
+    const FfnShape d(n, c_in, hidden, c_out);
+    if (!ffn_launches(dtype, d, false)) return fail(GSC_EINVAL, "gated_ffn_fwd: more rows and columns than a launch takes");
     if (n == 0) return GSC_OK;
     if (!X || !Wg || !Wu || !Wd || !Y) return fail(GSC_EINVAL, "gated_ffn_fwd: null X/Wg/Wu/Wd/Y");
-    const FfnShape d(n, c_in, hidden, c_out);
     const FfnLayout L = ffn_layout(dtype, d, false);
     if (!ws || ws_bytes < L.total)
         return fail(GSC_ESHORT, "gated_ffn_fwd: ws needs %zu bytes, got %zu", L.total, ws ? ws_bytes : (size_t)0);
@@ -962,13 +978,11 @@ int gsc_gated_ffn_bwd(int32_t dtype, const void* X, int64_t n, int32_t c_in, con
     if (!ffn_sizes_ok(dtype, n, c_in, hidden, c_out))
         return fail(GSC_EINVAL, "gated_ffn_bwd: bad sizes n=%lld c_in=%d hidden=%d c_out=%d", (long long)n, c_in, hidden,
                     c_out);
-    const int widest = hidden > c_out ? (hidden > c_in ? hidden : c_in) : (c_out > c_in ? c_out : c_in);
-    if (ceil_div(n, 64) * ceil_div(widest, 64) > 0x7fffffff)
-        return fail(GSC_EINVAL, "gated_ffn_bwd: more tiles than a launch takes");
+    const FfnShape d(n, c_in, hidden, c_out);
+    if (!ffn_launches(dtype, d, true)) return fail(GSC_EINVAL, "gated_ffn_bwd: more rows and columns than a launch takes");
     if (!dX && !dWg && !dWu && !dWd) return GSC_OK;
     if (n == 0 && !dWg && !dWu && !dWd) return GSC_OK;
     if (n > 0 && (!X || !Wg || !Wu || !Wd || !dY)) return fail(GSC_EINVAL, "gated_ffn_bwd: null X/Wg/Wu/Wd/dY");
-    const FfnShape d(n, c_in, hidden, c_out);
     const FfnLayout L = ffn_layout(dtype, d, true);
     if (!ws || ws_bytes < L.total)
         return fail(GSC_ESHORT, "gated_ffn_bwd: ws needs %zu bytes, got %zu", L.total, ws ? ws_bytes : (size_t)0);

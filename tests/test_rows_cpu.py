@@ -118,3 +118,21 @@ def test_layer_norm_wide_workspace(L):
     assert L.gsc_layer_norm_bwd_ws_bytes(7, 2048) == 2 * 2 * 2048 * 4
     assert L.gsc_layer_norm_bwd_ws_bytes(7, 2049) == 2 * 2 * 2049 * 4 + 3 * 7 * 4
     assert L.gsc_layer_norm_bwd_ws_bytes(10**7, 4096) == 1024 * 2 * 4096 * 4 + 3 * 10**7 * 4
+
+
+def test_gated_ffn_launch_sizes(L):
+    """A launch takes fewer than 2^32 threads: sizes that would ask for more are refused before anything is launched, the
+    ones just below are not (they come as far as the check of the workspace)."""
+    def call(dt, n, ci, f, co, bwd):
+        a = (dt, FAKE, n, ci, FAKE, FAKE, f, FAKE, co)
+        if not bwd:
+            return L.gsc_gated_ffn_fwd(*a, 0, FAKE, FAKE, 16, None)
+        return L.gsc_gated_ffn_bwd(*a, FAKE, 0, FAKE, FAKE, FAKE, FAKE, FAKE, 16, None)
+
+    top = 1 << 30
+    for dt, n, ci, f, co, bwd in ((gsc.GSC_BF16, top, 8, 8, 8, 0),            # rows in registers, 512 threads a tile
+                                  (gsc.GSC_F32, 2 * top, 8, 8, 8, 0),         # ... 256
+                                  (gsc.GSC_BF16, 2 * top, 8, 8, 8, 1),        # tiles by 64 columns
+                                  (gsc.GSC_F32, top, 200, 65, 65, 0), (gsc.GSC_BF16, top // 2, 64, 200, 8, 1)):
+        assert call(dt, n, ci, f, co, bwd) == gsc.GSC_EINVAL and "launch" in _err(L), (dt, n, bwd)
+        assert call(dt, n - 128, ci, f, co, bwd) == gsc.GSC_ESHORT, (dt, n, bwd)
