@@ -624,9 +624,11 @@ int gsc_rotary(int32_t dtype, const void* X, int64_t n, int32_t heads, int32_t d
  * bfloat16: products on bfloat16 operands with float32 sums; the hidden rows
  * act(X Wg) * (X Wu) are rounded to bfloat16 once between the two products.
  * A row of X with a NaN or an infinity gives NaN or infinite values in that
- * row alone.  ws: gsc_gated_ffn_fwd_ws_bytes bytes (hidden rows and, in
- * bfloat16, laid out weights and copies of unaligned rows), aligned to 16 bytes,
- * contents not kept; calls that may overlap need one each, and so does a
+ * row alone.  ws: gsc_gated_ffn_fwd_ws_bytes bytes on the device that takes the
+ * call (what its kernels use: many rows of at most 256 channels, float32 128,
+ * 256 bytes in float32 and the packed weights in bfloat16; else hidden rows and,
+ * in bfloat16, copies of unaligned matrices), aligned to 16 bytes, contents not
+ * kept; calls that may overlap need one each, and so does a
  * captured graph.  Asynchronous.  Errors: EINVAL, ESHORT (ws), EHIP. */
 typedef enum {
     GSC_GATE_SILU = 0,

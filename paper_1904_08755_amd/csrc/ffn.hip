@@ -602,8 +602,10 @@ struct FfnShape {
 };
 
 // Workspace, in order: what the padded copies of X, dY (backward), Wg, Wu and Wd and the packed weights take
-// (bfloat16), H, then for the backward pass dG | dU and the weight gradients' partial sums.
+// (bfloat16), H, then for the backward pass dG | dU and the weight gradients' partial sums; each only where the kernels
+// that take the call use it.  (The copies also for widths that need none: a call's addresses may.)
 struct FfnLayout {
+    bool few, res;      // k_ffn_few; rows in registers
     size_t x, dy, wg, wu, wd, pack, h, dgu, part, total;
     int64_t per_chunk, up, chunks, chunk;
     bool m_nar, n_nar;      // tiles of 64 channels for the weight gradients of the first, of the second projection
@@ -683,16 +685,19 @@ static FfnLayout ffn_layout(int dtype, const FfnShape& d, bool bwd) {
         return a;
     };
     const int64_t rows = d.n > 0 ? d.n : 1;
-    if (dtype == GSC_BF16) {
+    L.few = !bwd && d.n <= kFfnFewRows;
+    L.res = !L.few && ffn_res(dtype, d, bwd);
+    if (dtype == GSC_BF16 && (bwd || !(L.few || L.res))) {
         L.x = take((size_t)d.n * pad8(d.ci) * 2);
         if (bwd) L.dy = take((size_t)d.n * pad8(d.co) * 2);
         L.wg = take((size_t)d.ci * pad8(d.f) * 2);
         L.wu = take((size_t)d.ci * pad8(d.f) * 2);
-        L.wd = take((size_t)d.f * pad8(d.co) * 2);
-        if (ffn_res_can(d)) L.pack = take(res_pack_bytes(d.ci, d.f, d.co));
+        if (!L.res) L.wd = take((size_t)d.f * pad8(d.co) * 2);
     }
+    if (dtype == GSC_BF16 && L.res) L.pack = take(res_pack_bytes(d.ci, d.f, d.co));
     const int64_t tiles = ceil_div(d.n, 128);
-    L.h = take((size_t)(!bwd && d.n <= kFfnFewRows ? d.n * 4 : tiles * 128 * size) * d.fp);
+    if (L.few) L.h = take((size_t)d.n * 4 * d.fp);
+    else if (bwd || !L.res) L.h = take((size_t)tiles * 128 * size * d.fp);
     if (bwd) {
         L.dgu = take((size_t)tiles * 128 * 2 * d.fp * size);
         int bm0, bn0, bm1, bn1;
@@ -751,7 +756,7 @@ static void ffn_gemm_f32(RowMat<const float> A1, RowMat<const float> A2, int64_t
 
 static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const float* X, const float* Wg, const float* Wu,
                     const float* Wd, int act, float* Y, char* ws, hipStream_t s) {
-    if (ffn_res_f32(d, false)) return res_fwd(X, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, Y, s);
+    if (L.res) return res_fwd(X, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, Y, s);
     const RowMat<float> H = row_blocks(reinterpret_cast<float*>(ws + L.h), d.fp);
     const int nf = (int)ceil_div(d.f, 64);
     const bool sho = ffn_short(d.n, 128, nf);
@@ -764,10 +769,10 @@ static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const float* X, const
     });
 }
 
-static void ffn_bwd_rows(const FfnShape& d, const float* X, const float* Wg, const float* Wu, const float* Wd,
+static void ffn_bwd_rows(const FfnShape& d, const FfnLayout& L, const float* X, const float* Wg, const float* Wu, const float* Wd,
                          const float* dY, int act, float* dX, RowMat<float> H, RowMat<float> dG, RowMat<float> dU,
                          hipStream_t s) {
-    if (ffn_res_f32(d, true)) return res_bwd(X, dY, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, (int)d.fp, H, dG, dU, dX, s);
+    if (L.res) return res_bwd(X, dY, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, (int)d.fp, H, dG, dU, dX, s);
     const int nf = (int)ceil_div(d.f, 64);
     const bool sho = ffn_short(d.n, 128, nf);
     ffn_whole(d, [&](auto WHOLE) {
@@ -825,11 +830,8 @@ static void ffn_gemm_bf16(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, 
 
 static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const uint16_t* X, const uint16_t* Wg, const uint16_t* Wu,
                     const uint16_t* Wd, int act, uint16_t* Y, char* ws, hipStream_t s) {
+    if (L.res) return res_fwd(X, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, Y, ws + L.pack, s);
     const RowMat<uint16_t> H = row_blocks(reinterpret_cast<uint16_t*>(ws + L.h), d.fp);
-    if (ffn_res_fwd(d)) {
-        res_fwd(X, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, Y, ws + L.pack, s);
-        return;
-    }
     FfnPad pad{};
     const FfnMat x = ffn_mat(X, d.n, d.ci, ws + L.x, pad), g = ffn_mat(Wg, d.ci, d.f, ws + L.wg, pad),
                  u = ffn_mat(Wu, d.ci, d.f, ws + L.wu, pad), w = ffn_mat(Wd, d.f, d.co, ws + L.wd, pad);
@@ -894,14 +896,14 @@ static void ffn_bwd(const FfnShape& d, const FfnLayout& L, const T* X, const T* 
             FfnPad pad{};
             const FfnMat x = ffn_mat(X, n, d.ci, ws + L.x, pad), y = ffn_mat(dY, n, d.co, ws + L.dy, pad),
                          g = ffn_mat(Wg, d.ci, d.f, ws + L.wg, pad), u = ffn_mat(Wu, d.ci, d.f, ws + L.wu, pad),
-                         w = ffn_mat(Wd, d.f, d.co, ws + L.wd, pad);
+                         w = L.res ? FfnMat{} : ffn_mat(Wd, d.f, d.co, ws + L.wd, pad);
             ffn_pad(pad, s);
             xs = x.p;
             ys = y.p;
             ldx = x.ld;
             ldy = y.ld;
             const int nf = (int)ceil_div(d.f, 64);
-            if (ffn_res_bwd(d)) {
+            if (L.res) {
                 res_mid(X, dY, n, d.ci, Wg, Wu, d.f, Wd, d.co, act, H, dG, dU, ws + L.pack, s);
             } else {
                 hipLaunchKernelGGL(k_ffn_mid_bf16<4>, dim3((unsigned)(ceil_div(n, 128) * nf)), dim3(256), 0, s, x.p, x.ld,
@@ -909,7 +911,7 @@ static void ffn_bwd(const FfnShape& d, const FfnLayout& L, const T* X, const T* 
             }
             if (dX) ffn_dx_bf16(ffn_const(dG), ffn_const(dU), n, d.f, g.p, u.p, g.ld, d.ci, dX, s);
         } else {
-            ffn_bwd_rows(d, X, Wg, Wu, Wd, dY, act, dX, H, dG, dU, s);
+            ffn_bwd_rows(d, L, X, Wg, Wu, Wd, dY, act, dX, H, dG, dU, s);
         }
     }
     if (!dWg && !dWu && !dWd) return;
@@ -955,7 +957,7 @@ int gsc_gated_ffn_fwd(int32_t dtype, const void* X, int64_t n, int32_t c_in, con
     auto run = [&](auto t) {
         typedef decltype(t) T;
         const T *x = (const T*)X, *g = (const T*)Wg, *u = (const T*)Wu, *w = (const T*)Wd;
-        if (n <= kFfnFewRows) ffn_fwd_few<T>(d, L, x, g, u, w, act, (T*)Y, (char*)ws, s);
+        if (L.few) ffn_fwd_few<T>(d, L, x, g, u, w, act, (T*)Y, (char*)ws, s);
         else ffn_fwd(d, L, x, g, u, w, act, (T*)Y, (char*)ws, s);
     };
     if (dtype == GSC_BF16) run(uint16_t{});

@@ -959,3 +959,22 @@ def test_layer_norm_widest_rows():
     _close(dX, refs[0], bounds[0] * 1.01 + HALF[torch.bfloat16] * refs[0].abs() * 1.01, "dX")
     _close(dgamma, refs[1], bounds[1] * 1.01, "dgamma")
     _close(dbeta, refs[2], bounds[2] * 1.01, "dbeta")
+
+
+@pytest.mark.parametrize("dtype,n,ci,f,co,at", [
+    (torch.bfloat16, 1, 100, 267, 90, 1), (torch.bfloat16, 4, 64, 256, 64, 0), (torch.bfloat16, 5, 33, 50, 7, 1),
+    (torch.bfloat16, 1000, 300, 90, 129, 1), (torch.bfloat16, 13001, 99, 130, 64, 1), (torch.bfloat16, 33001, 256, 200, 256, 0),
+    (torch.bfloat16, 90001, 128, 512, 96, 1), (torch.float32, 3, 100, 267, 90, 1), (torch.float32, 200, 31, 70, 29, 1),
+    (torch.float32, 200, 65, 70, 29, 0), (torch.float32, 32700, 64, 256, 64, 0), (torch.float32, 33001, 130, 67, 33, 1)])
+def test_gated_ffn_workspace_of_the_stated_size(dtype, n, ci, f, co, at):
+    """Workspaces of exactly the stated size, filled with NaN: nothing behind them is written, nothing depends on what
+    they held."""
+    X, Wg, Wu, Wd, dY = _ffn_inputs(dtype, n, ci, f, co, at)
+    want = gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd), *gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY)
+    L, dt = gsc.lib(), gsc._dt(X)
+    sizes = L.gsc_gated_ffn_fwd_ws_bytes(dt, n, ci, f, co), L.gsc_gated_ffn_bwd_ws_bytes(dt, n, ci, f, co)
+    bufs = [torch.full((s + 8192,), 255, dtype=torch.uint8, device=DEV) for s in sizes]
+    got = (gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd, ws=bufs[0][:sizes[0]]),
+           *gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, ws=bufs[1][:sizes[1]]))
+    assert all(torch.equal(p, q) for p, q in zip(got, want))
+    assert all((b[s:] == 255).all() for b, s in zip(bufs, sizes))

@@ -136,3 +136,23 @@ def test_gated_ffn_launch_sizes(L):
                                   (gsc.GSC_F32, top, 200, 65, 65, 0), (gsc.GSC_BF16, top // 2, 64, 200, 8, 1)):
         assert call(dt, n, ci, f, co, bwd) == gsc.GSC_EINVAL and "launch" in _err(L), (dt, n, bwd)
         assert call(dt, n - 128, ci, f, co, bwd) == gsc.GSC_ESHORT, (dt, n, bwd)
+
+
+def test_gated_ffn_workspace_is_what_the_kernels_use(L):
+    """Upper bounds (256 bytes of padding a part): no hidden rows where they stay in registers, no copies where nothing is
+    copied, one float32 hidden row each for a few rows.  (Without a device the library takes it to have 256 compute units.)"""
+    fwd, bwd, B, F = L.gsc_gated_ffn_fwd_ws_bytes, L.gsc_gated_ffn_bwd_ws_bytes, gsc.GSC_BF16, gsc.GSC_F32
+    assert fwd(B, 300_000, 256, 1024, 256) <= 3 * 256 * 1024 * 2 + 256         # the packed weights (771 MB with all parts)
+    assert fwd(F, 120_011, 64, 256, 64) <= 256
+    assert fwd(B, 13_000, 100, 267, 100) <= 3 * 128 * 320 * 2 + 256
+    for n in (1, 4):
+        assert fwd(B, n, 256, 1024, 256) <= n * 1024 * 4 + 256
+        assert fwd(F, n, 256, 1024, 256) <= n * 1024 * 4 + 256
+    # tiles: X, the weights and the hidden rows
+    assert fwd(B, 1000, 300, 90, 129) <= 1000 * 304 * 2 + 2 * 300 * 96 * 2 + 90 * 136 * 2 + 1024 * 128 * 2 + 5 * 256
+    assert fwd(F, 1000, 300, 90, 129) <= 1024 * 128 * 4 + 256
+    # backward: X, dY and the projections' copies, hidden rows three times, at most 512 chunks' sums
+    part = (256 * 2048 + 1024 * 256) * 4
+    hid = 300_032 * 1024 * 2
+    assert bwd(B, 300_000, 256, 1024, 256) <= 2 * 300_000 * 512 + 2 * 2**19 + 3 * 2**19 + 3 * hid + 64 * part + 8 * 256
+    assert bwd(F, 1000, 64, 256, 64) <= 3 * 1024 * 256 * 4 + 8 * (64 * 512 + 256 * 64) * 4 + 3 * 256
