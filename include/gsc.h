@@ -622,7 +622,10 @@ int gsc_rotary(int32_t dtype, const void* X, int64_t n, int32_t heads, int32_t d
  * |g| for SILU and SIGMOID, 1.25 g^2 for GELU (bfloat16: 16 more), 6 |2 sqrt(2 /
  * pi) (g + 0.044715 g^3)| for GELU_TANH.
  * bfloat16: products on bfloat16 operands with float32 sums; the hidden rows
- * act(X Wg) * (X Wu) are rounded to bfloat16 once between the two products.
+ * act(X Wg) * (X Wu) are rounded to bfloat16 once between the two products, as
+ * the matrix cores take them; calls of up to 4 rows do not use those and keep
+ * them in float32, so a row's last digit may differ between a call of few rows
+ * and one of many.
  * A row of X with a NaN or an infinity gives NaN or infinite values in that
  * row alone.  ws: gsc_gated_ffn_fwd_ws_bytes bytes on the device that takes the
  * call (what its kernels use: many rows of at most 256 channels, float32 128,

@@ -14,8 +14,8 @@
 // The weights' gradients are k_ffn_dw over row chunks and k_ffn_dw_sum, which adds the chunks in order: every result is
 // bit-reproducible.
 //
-// bfloat16: G, U, dH and all sums stay in float32; H, dG and dU are rounded to bfloat16 once, as the matrix cores take them, and
-// the results once as they are stored.  Its tiles copy operands straight into LDS (ffn_bf16.h), which takes rows of whole
+// bfloat16: G, U, dH and all sums stay in float32; H (but for a few rows), dG and dU are rounded to bfloat16 once, as the
+// matrix cores take them, and the results once as they are stored.  Its tiles copy operands straight into LDS (ffn_bf16.h), which takes rows of whole
 // 16-byte pieces at 16-byte addresses: operands that are not are copied into the workspace first, their rows padded with zeros
 // (k_ffn_pad; the weights and at most two passes over rows, against kernels that would load element by element).  float32
 // tiles (ffn_f32.h) take any address.
@@ -863,7 +863,7 @@ static void ffn_dx_bf16(RowMat<const uint16_t> dG, RowMat<const uint16_t> dU, in
 }
 
 // --- either type
-// A few rows: H in float32.
+// A few rows: H in float32 (no matrix core takes it, and it stays in the L2).
 template <typename T>
 static void ffn_fwd_few(const FfnShape& d, const FfnLayout& L, const T* X, const T* Wg, const T* Wu, const T* Wd, int act,
                         T* Y, char* ws, hipStream_t s) {

@@ -978,3 +978,26 @@ def test_gated_ffn_workspace_of_the_stated_size(dtype, n, ci, f, co, at):
            *gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, ws=bufs[1][:sizes[1]]))
     assert all(torch.equal(p, q) for p, q in zip(got, want))
     assert all((b[s:] == 255).all() for b, s in zip(bufs, sizes))
+
+
+def test_gated_ffn_hidden_rows_few_and_more():
+    """bfloat16: up to 4 rows the hidden rows stay in float32, from 5 on they are rounded to bfloat16."""
+    ci, f, co = 96, 200, 64
+    X, Wg, Wu, Wd, _ = _ffn_inputs(torch.bfloat16, 5, ci, f, co)
+    x, wg, wu, wd = (t.double() for t in (X, Wg, Wu, Wd))
+    G, Up = x @ wg, x @ wu
+    eG, eU = ((ci + 2) * U * (x.abs() @ w.abs()) for w in (wg, wu))
+    (a, _), (e_a, _) = _act_digits("silu", G)
+    H = a * Up
+    eH = (e_a + 1.13 * eG) * (Up.abs() + eU) + a.abs() * eU + 2 * U * H.abs()
+    low = H.to(torch.bfloat16).double()
+    # a value whose neighbours within eH round to other sides may go either way
+    either = ((H - eH).to(torch.bfloat16).double() - (H + eH).to(torch.bfloat16).double()).abs()
+    for n, h, e in ((4, H, eH), (5, low, either)):
+        Y = gsc.gsc_gated_ffn_fwd(X[:n].contiguous(), Wg, Wu, Wd)
+        y = (h @ wd)[:n]
+        bound = (e @ wd.abs() + (f + 2) * U * ((h.abs() + e) @ wd.abs()))[:n]
+        _close(Y, y, bound * 1.01 + HALF[torch.bfloat16] * (y.abs() + bound), n)
+        # ... and the other rule's values are not these
+        other = ((low if n == 4 else H) @ wd)[:n]
+        assert (Y.double() - y).norm() < 0.9 * (Y.double() - other).norm(), n
