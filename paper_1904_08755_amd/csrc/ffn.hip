@@ -319,13 +319,13 @@ k_ffn_gemm_bf16(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n,
     store_tile(acc, r0 + 16 * MT * (wave / WN), c0 + 64 * (wave % WN), n, co, Out, co);
 }
 
-// Out (n x co) = A1 B1 + A2 B2 for KC operands in tiles of 256 x 256: eight waves of 64 x 128 (v_mfma_f32_32x32x16_bf16), a
+// Out (n x co, at most 256) = A1 B1 + A2 B2 for KC operands in tiles of 256 x 256: eight waves of 64 x 128 (v_mfma_f32_32x32x16_bf16), a
 // ring of four stages of 32 reduction elements, each an array of its own: the operands are plain reads, which the compiler
 // starts ahead of the products without waiting for copies into other stages.  Bound: about as much time in the copies as in
 // the products (300,000 rows, 256 columns, 2 x 1,024 elements: 391 us; without the copies 288, without the products 368).
 __global__ void __launch_bounds__(512, 1)
 k_ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, int64_t k, const uint16_t* __restrict__ B1,
-              const uint16_t* __restrict__ B2, int64_t ldb, int co, uint16_t* __restrict__ Out, int nc) {
+              const uint16_t* __restrict__ B2, int64_t ldb, int co, uint16_t* __restrict__ Out) {
     constexpr int TN = 4;   // 32-column tiles of a wave
     constexpr int BN = 64 * TN, STAGE = (256 + BN) * 64;
     typedef FbCopy<FB_KC, 256, 8, true> CA;
@@ -339,12 +339,10 @@ k_ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, i
         constexpr int s = decltype(N)::value % 4;
         return s == 0 ? slot0 : (s == 1 ? slot1 : (s == 2 ? slot2 : slot3));
     };
-    const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
-    const int64_t r0 = u / nc * 256;
-    const int c0 = (int)(u % nc) * BN;
+    const int64_t r0 = xcd_unit(blockIdx.x, gridDim.x) * 256;
     const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), wm = wave >> 1, wn = wave & 1;
     const FbSide a1{A1.at(r0, 0), n - r0}, a2{A2.at(r0, 0), n - r0};
-    const FbSide b1{row_major(B1 + (int64_t)c0 * ldb, ldb), co - c0}, b2{row_major(B2 + (int64_t)c0 * ldb, ldb), co - c0};
+    const FbSide b1{row_major(B1, ldb), co}, b2{row_major(B2, ldb), co};
     CA ca;
     CB cb;
     ca.start(a1, wave);
@@ -413,7 +411,7 @@ k_ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, i
             uint32_t o[8];
 #pragma unroll
             for (int e = 0; e < 8; ++e) o[e] = pack_bf16(acc[m][t][2 * e], acc[m][t][2 * e + 1]);
-            res_store<false>(Out, co, r0 + 64 * wm + 32 * m, n, c0 + 32 * (TN * wn + t), co, o);
+            res_store<false>(Out, co, r0 + 64 * wm + 32 * m, n, 32 * (TN * wn + t), co, o);
         }
 }
 // H, dG and dU of a tile of 128 rows by 64 hidden columns.
@@ -852,14 +850,20 @@ static void ffn_dw(const FfnShape& d, const FfnLayout& L, const DwSide<uint16_t>
                        L.per_chunk, part);
 }
 
-// Tiles of 256 x 256 where they fill the device and are not mostly empty (60,000 rows of 256 channels, 1,024 hidden: 27 us of
-// the whole backward pass; no difference at 128 channels).
+// Tiles of 256 x 256, a block a compute unit, for one tile of columns that is more than half full, at least 768 hidden columns
+// (less, and filling the pipeline costs what the shared operands save) and blocks that fill an eighth less than
+// whole rounds of the device or more.  dH, dG, dU and dX of 256 channels, 64 outputs, such tiles and the others: 1,024 hidden
+// 60,000 rows 242 and 272 us, 300,000 1,070 and 1,080, but 90,000 rows (1.4 rounds) 345 and 338, 33,000 (half a round) 125 and
+// 128 (160 channels 109 and 104); 512 hidden 300,000 rows 597 and 589.  Two tiles of columns: 264 channels, 60,000 rows, 1,024
+// hidden 296 and 291, 300,000 rows 1,450 and 1,339; 512 channels 356 and 367, 1,748 and 1,728.  128 channels: no difference.
+static bool ffn_dx_wide(int64_t n, int64_t f, int ci) {
+    const int64_t blocks = ceil_div(n, 256), cus = device_cus();
+    return ci > 128 && ci <= 256 && f >= 768 && 8 * blocks >= 7 * ceil_div(blocks, cus) * cus;
+}
 static void ffn_dx_bf16(RowMat<const uint16_t> dG, RowMat<const uint16_t> dU, int64_t n, int64_t f, const uint16_t* Wg,
                         const uint16_t* Wu, int64_t ldw, int ci, uint16_t* dX, hipStream_t s) {
-    if (ci <= 128 || n < 256 * 128) return ffn_gemm_bf16<FB_KC>(dG, dU, n, f, Wg, Wu, ldw, ci, dX, s);
-    const int nc = (int)ceil_div(ci, 256);
-    hipLaunchKernelGGL(k_ffn_gemm_kc, dim3((unsigned)(ceil_div(n, 256) * nc)), dim3(512), 0, s, dG, dU, n, f, Wg, Wu, ldw, ci,
-                       dX, nc);
+    if (!ffn_dx_wide(n, f, ci)) return ffn_gemm_bf16<FB_KC>(dG, dU, n, f, Wg, Wu, ldw, ci, dX, s);
+    hipLaunchKernelGGL(k_ffn_gemm_kc, dim3((unsigned)ceil_div(n, 256)), dim3(512), 0, s, dG, dU, n, f, Wg, Wu, ldw, ci, dX);
 }
 
 // --- either type

@@ -1001,3 +1001,26 @@ def test_gated_ffn_hidden_rows_few_and_more():
         # ... and the other rule's values are not these
         other = ((low if n == 4 else H) @ wd)[:n]
         assert (Y.double() - y).norm() < 0.9 * (Y.double() - other).norm(), n
+
+
+# the input gradient's tiles of 256 x 256: a column more and a hidden column less than they take, rows on both sides of
+# a filled round, odd widths and addresses
+@pytest.mark.parametrize("n,ci,f,co,at", [(60001, 256, 768, 40, 0), (60001, 129, 1030, 8, 1), (60011, 257, 768, 24, 0),
+                                          (60001, 256, 767, 33, 0), (66001, 200, 800, 64, 0), (33001, 256, 800, 8, 0)])
+def test_gated_ffn_input_gradient_tiles(n, ci, f, co, at):
+    X, Wg, Wu, Wd, dY = _ffn_inputs(torch.bfloat16, n, ci, f, co, at)
+    dX = gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, need_dw=False)[0]
+    for sl in (slice(0, 3000), slice(n - 3000, n)):
+        x, dy = X[sl].contiguous(), dY[sl].contiguous()
+        _ffn_check(x, Wg, Wu, Wd, dy, "silu", None, (dX[sl].contiguous(), None, None, None))
+    assert torch.equal(gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY)[0], dX)
+
+
+def test_gated_ffn_input_gradient_past_32_bits():
+    """dG and dU of more than 2^32 elements under the tiles of 256 x 256."""
+    n, ci, f, co = (1 << 21) + 77, 200, 1040, 8
+    X, Wg, Wu, Wd, dY = _ffn_inputs(torch.bfloat16, n, ci, f, co)
+    dX = gsc.gsc_gated_ffn_bwd(X, Wg, Wu, Wd, dY, need_dw=False)[0]
+    for sl in (slice(0, 200), slice(n // 2, n // 2 + 200), slice(n - 200, n)):
+        x, dy = X[sl].contiguous(), dY[sl].contiguous()
+        _ffn_check(x, Wg, Wu, Wd, dy, "silu", None, (dX[sl].contiguous(), None, None, None))
