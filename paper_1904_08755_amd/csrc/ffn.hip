@@ -619,13 +619,16 @@ static bool ffn_fills(int64_t n) {
 // Whether the kernels that keep rows in registers can take a bfloat16 call at all.
 static bool ffn_res_can(const FfnShape& d) { return d.ci <= kResMax && d.co <= kResMax; }
 
-// ... and do.  Forward, up to 128 channels: from about 100 tiles of 128 rows on (16,000 rows of 128 channels 20 us, tiles 21; of
-// 100 channels, which tiles have to copy first, 14 and 21; 8,000 rows of 128 channels 19 and 16).  Wider ones take a block a
+// ... and do.  Forward, up to 64 channels: from 40 tiles of 128 rows on (64 channels, 1,024 hidden: 4,000 rows 23.0 us, tiles
+// 21.6; 6,000 rows 23.0 and 23.3; 12,000 rows 23.0 and 27.8; 256 hidden: 4,000 rows 10.8 and 10.9, 12,000 rows 10.9 and 12.0; 32
+// channels alike, 8 and 16 no difference).  Up to 128 channels: from 100 tiles on (128 channels, 512 hidden: 10,000 rows 19.0
+// and 17.8, 14,000 rows 19.2 and 20.6; 96 channels: 10,000 rows 15.0 and 14.4, 14,000 rows 15.2 and 16.0).  Wider ones take a block a
 // compute unit: where they fill their rounds (256 channels: 30,000 rows 55 and 61 us, 45,000 rows in a second round of 96
 // blocks 96 and 84, 60,000 rows 102 and 112).
 static bool ffn_res_fwd(const FfnShape& d) {
     if (!ffn_res_can(d)) return false;
-    return d.ci <= 128 && d.co <= 128 ? ceil_div(d.n, 128) >= 100 : ffn_fills(d.n);
+    const int c = d.ci > d.co ? d.ci : d.co;
+    return c > 128 ? ffn_fills(d.n) : ceil_div(d.n, 128) >= (c > 64 ? 100 : 40);
 }
 // Backward: once H, dG and dU outgrow the 256 MB of the last-level cache, where the tiles' traffic costs more than their better
 // spread over the device saves (forward and backward of 128 channels, 512 hidden: 60,000 rows 155 us, tiles 148; 90,000 rows

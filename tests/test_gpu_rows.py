@@ -1024,3 +1024,12 @@ def test_gated_ffn_input_gradient_past_32_bits():
     for sl in (slice(0, 200), slice(n // 2, n // 2 + 200), slice(n - 200, n)):
         x, dy = X[sl].contiguous(), dY[sl].contiguous()
         _ffn_check(x, Wg, Wu, Wd, dy, "silu", None, (dX[sl].contiguous(), None, None, None))
+
+
+@pytest.mark.parametrize("n,ci,f,co,at", [(4992, 64, 256, 64, 0), (4993, 64, 256, 64, 0), (5001, 33, 70, 64, 1),
+                                          (4999, 65, 100, 30, 0), (6003, 8, 32, 3, 1), (12673, 128, 96, 65, 0)])
+def test_gated_ffn_forward_rows_in_registers_from(n, ci, f, co, at):
+    """bfloat16, both sides of the row counts from which the forward pass keeps rows in registers."""
+    X, Wg, Wu, Wd, dY = _ffn_inputs(torch.bfloat16, n, ci, f, co, at)
+    for act in ACTS:
+        _ffn_check(X, Wg, Wu, Wd, dY, act, gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd, act), None)

@@ -156,3 +156,13 @@ def test_gated_ffn_workspace_is_what_the_kernels_use(L):
     hid = 300_032 * 1024 * 2
     assert bwd(B, 300_000, 256, 1024, 256) <= 2 * 300_000 * 512 + 2 * 2**19 + 3 * 2**19 + 3 * hid + 64 * part + 8 * 256
     assert bwd(F, 1000, 64, 256, 64) <= 3 * 1024 * 256 * 4 + 8 * (64 * 512 + 256 * 64) * 4 + 3 * 256
+
+
+def test_gated_ffn_rows_in_registers_from(L):
+    """The forward pass of at most 64 channels writes no hidden rows from 40 tiles of 128 rows on, of at most 128 from 100."""
+    size = L.gsc_gated_ffn_fwd_ws_bytes
+    for c, tiles in ((8, 40), (64, 40), (65, 100), (128, 100)):
+        n = 128 * (tiles - 1)
+        pack = 3 * (64 if c <= 64 else 128) * 256 * 2
+        assert size(gsc.GSC_BF16, n, c, 256, 8) > n * 256 * 2 and size(gsc.GSC_BF16, n + 1, c, 256, 8) == pack, c
+        assert size(gsc.GSC_BF16, n, 8, 256, c) > n * 256 * 2 and size(gsc.GSC_BF16, n + 1, 8, 256, c) == pack, c
