@@ -414,13 +414,14 @@ k_ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, i
             res_store<false>(Out, co, r0 + 64 * wm + 32 * m, n, 32 * (TN * wn + t), co, o);
         }
 }
+
 // H, dG and dU of a tile of 128 rows by 64 hidden columns.
-template <int MT>
 __global__ void __launch_bounds__(256, 2)
 k_ffn_mid_bf16(const uint16_t* __restrict__ X, int64_t ldx, const uint16_t* __restrict__ dY, int64_t ldy, int64_t n, int ci,
                int co, const uint16_t* __restrict__ Wg, const uint16_t* __restrict__ Wu, int64_t ldw,
                const uint16_t* __restrict__ Wd, int64_t ldd, int f, int act, RowMat<uint16_t> H, RowMat<uint16_t> dG,
                RowMat<uint16_t> dU, int nf) {
+    constexpr int MT = 4;
     typedef FbShape<2, 2, MT, 4> S;
     __shared__ __attribute__((aligned(1024))) uint8_t lds[S::LDS];
     const int64_t u = xcd_unit(blockIdx.x, gridDim.x);
@@ -913,7 +914,7 @@ static void ffn_bwd(const FfnShape& d, const FfnLayout& L, const T* X, const T* 
             if (L.res) {
                 res_mid(X, dY, n, d.ci, Wg, Wu, d.f, Wd, d.co, act, H, dG, dU, ws + L.pack, s);
             } else {
-                hipLaunchKernelGGL(k_ffn_mid_bf16<4>, dim3((unsigned)(ceil_div(n, 128) * nf)), dim3(256), 0, s, x.p, x.ld,
+                hipLaunchKernelGGL(k_ffn_mid_bf16, dim3((unsigned)(ceil_div(n, 128) * nf)), dim3(256), 0, s, x.p, x.ld,
                                    y.p, y.ld, n, d.ci, d.co, g.p, u.p, g.ld, w.p, w.ld, d.f, act, H, dG, dU, nf);
             }
             if (dX) ffn_dx_bf16(ffn_const(dG), ffn_const(dU), n, d.f, g.p, u.p, g.ld, d.ci, dX, s);
