@@ -740,6 +740,8 @@ _current_raw = getattr(torch._C, "_cuda_getCurrentRawStream", None)
 
 def _raw_stream(stream, device: int) -> int:
     if stream is not None:
+        if stream.device_index != device:
+            raise ValueError(f"the stream is on cuda:{stream.device_index}, the tensors on cuda:{device}")
         return stream.cuda_stream
     return torch.cuda.current_stream(device).cuda_stream if _current_raw is None else _current_raw(device)
 

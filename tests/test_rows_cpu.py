@@ -166,3 +166,12 @@ def test_gated_ffn_rows_in_registers_from(L):
         pack = 3 * (64 if c <= 64 else 128) * 256 * 2
         assert size(gsc.GSC_BF16, n, c, 256, 8) > n * 256 * 2 and size(gsc.GSC_BF16, n + 1, c, 256, 8) == pack, c
         assert size(gsc.GSC_BF16, n, 8, 256, c) > n * 256 * 2 and size(gsc.GSC_BF16, n + 1, 8, 256, c) == pack, c
+
+
+def test_stream_of_another_device_is_refused():
+    class Stream:
+        cuda_stream, device_index = 0x40, 1
+
+    assert gsc._raw_stream(Stream(), 1) == 0x40
+    with pytest.raises(ValueError, match="cuda:1"):
+        gsc._raw_stream(Stream(), 0)
