@@ -638,12 +638,15 @@ static bool ffn_res_bwd(const FfnShape& d) {
     return ffn_res_can(d) && (d.ci > 64 || d.co > 64) && d.n * d.fp * 6 >= (int64_t)256 << 20;
 }
 
-// float32: where the blocks fill their rounds (64 channels, 256 hidden, forward and backward: 16,000 rows 119 us, tiles 95;
-// 32,000 rows 141 and 156; 45,000 rows 215 and 207; 60,000 rows 227 and 259); forward always up to 32 channels, which
-// are few products a chunk (1,000 rows 11.1 and 11.4 us, 45,000 rows 18 and 25).
+// float32: where the blocks fill their rounds (64 channels, 256 hidden, forward 16,000 rows 31 us, tiles 26; 32,000 rows 32
+// and 41; 60,000 rows 55 and 70; backward 89 and 71, 110 and 116, 172 and 187, but 45,000 rows 162 and 150).  Forward of up to 32
+// channels, of which a compute unit takes several blocks: up to 128 hidden columns always (300 to 8,000 rows 10.5 to 10.8
+// us, tiles 10.8 to 11.2; 45,000 rows 18 and 25), more of them, which a block walks over one chunk after the other, from 150 tiles
+// on (256 hidden: 1,000 rows 18.6 us, tiles 13.1, 16,000 rows 18.9 and 20.3, 24,000 rows 19.5 and 27.8; 1,024 hidden: 65 and 33,
+// 68 and 59, 67 and 86; 45,000 rows 111 and 136).
 static bool ffn_res_f32(const FfnShape& d, bool bwd) {
     if (d.ci > kResMaxF32 || d.co > kResMaxF32) return false;
-    return ffn_fills(d.n) || (!bwd && d.ci <= 32 && d.co <= 32);
+    return ffn_fills(d.n) || (!bwd && d.ci <= 32 && d.co <= 32 && (d.f <= 128 || ceil_div(d.n, 128) >= 150));
 }
 
 // Which of the two ways a call of either type and pass goes.

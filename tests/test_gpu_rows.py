@@ -1080,3 +1080,12 @@ def test_gated_ffn_roundings_together(n, ci, f, co, act):
         err = (out.double() - ref).norm()
         print(name, float(err / want), float(err / ref.norm()))
         assert err <= 1.1 * want, (name, float(err / want))
+
+
+@pytest.mark.parametrize("n,ci,f,co,at", [(9, 32, 128, 32, 0), (9, 32, 129, 32, 0), (1001, 30, 513, 9, 1),
+                                          (19072, 32, 256, 16, 0), (19073, 32, 256, 16, 0), (19201, 7, 300, 31, 1)])
+def test_gated_ffn_float32_few_channels(n, ci, f, co, at):
+    """float32 of at most 32 channels, both sides of where the forward pass keeps rows in registers."""
+    X, Wg, Wu, Wd, dY = _ffn_inputs(torch.float32, n, ci, f, co, at)
+    for act in ACTS:
+        _ffn_check(X, Wg, Wu, Wd, dY, act, gsc.gsc_gated_ffn_fwd(X, Wg, Wu, Wd, act), None)

@@ -175,3 +175,12 @@ def test_stream_of_another_device_is_refused():
     assert gsc._raw_stream(Stream(), 1) == 0x40
     with pytest.raises(ValueError, match="cuda:1"):
         gsc._raw_stream(Stream(), 0)
+
+
+def test_gated_ffn_float32_rows_in_registers_from(L):
+    """The float32 forward pass of at most 32 channels writes no hidden rows up to 128 hidden columns, and from 150 tiles of
+    128 rows on; one of 64 channels where the tiles fill three quarters of a round of 256 compute units."""
+    size = lambda n, c, f: L.gsc_gated_ffn_fwd_ws_bytes(gsc.GSC_F32, n, c, f, 8)
+    assert size(5, 32, 128) == 256 and size(5, 32, 129) > 256 and size(5, 33, 128) > 256
+    assert size(128 * 149, 32, 512) > 128 * 149 * 512 * 4 - 1 and size(128 * 149 + 1, 32, 512) == 256
+    assert size(128 * 191, 64, 512) > 256 and size(128 * 192, 64, 512) == 256 and size(128 * 257, 64, 512) > 256
