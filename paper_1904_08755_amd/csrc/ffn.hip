@@ -229,7 +229,7 @@ __device__ __forceinline__ void dw_tile_f32(const DwSide<float>& p, int t, int64
 }
 
 // Partial sums of both products over the rows of a chunk, in tiles of 32 M0 channels by 128 hidden columns and of 128 hidden
-// columns by 32 N1 channels.  120,011 rows, 64 channels, 256 hidden: 145 us (tiles of 64 x 64: 166), the matrix cores
+// columns by 32 N1 channels.  120,011 rows, 64 channels, 256 hidden: 138 us (tiles of 64 x 64: 166), the matrix cores
 // busy 59 % of it; more blocks change nothing, what counts is the 447 MB from beyond the L2s.
 template <int M0, int N1, bool WHOLE>
 __global__ void __launch_bounds__(kFfnThreads, 2)
@@ -322,7 +322,7 @@ k_ffn_gemm_bf16(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n,
 // Out (n x co, at most 256) = A1 B1 + A2 B2 for KC operands in tiles of 256 x 256: eight waves of 64 x 128 (v_mfma_f32_32x32x16_bf16), a
 // ring of four stages of 32 reduction elements, each an array of its own: the operands are plain reads, which the compiler
 // starts ahead of the products without waiting for copies into other stages.  Bound: about as much time in the copies as in
-// the products (300,000 rows, 256 columns, 2 x 1,024 elements: 391 us; without the copies 288, without the products 368).
+// the products (300,000 rows, 256 columns, 2 x 1,024 elements: 385 us; without the copies 288, without the products 368).
 __global__ void __launch_bounds__(512, 1)
 k_ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, int64_t k, const uint16_t* __restrict__ B1,
               const uint16_t* __restrict__ B2, int64_t ldb, int co, uint16_t* __restrict__ Out) {
@@ -624,16 +624,17 @@ static bool ffn_res_can(const FfnShape& d) { return d.ci <= kResMax && d.co <= k
 // 21.6; 6,000 rows 23.0 and 23.3; 12,000 rows 23.0 and 27.8; 256 hidden: 4,000 rows 10.8 and 10.9, 12,000 rows 10.9 and 12.0; 32
 // channels alike, 8 and 16 no difference).  Up to 128 channels: from 100 tiles on (128 channels, 512 hidden: 10,000 rows 19.0
 // and 17.8, 14,000 rows 19.2 and 20.6; 96 channels: 10,000 rows 15.0 and 14.4, 14,000 rows 15.2 and 16.0).  Wider ones take a block a
-// compute unit: where they fill their rounds (256 channels: 30,000 rows 55 and 61 us, 45,000 rows in a second round of 96
-// blocks 96 and 84, 60,000 rows 102 and 112).
+// compute unit: where they fill their rounds (256 channels: 30,000 rows 57 and 62 us, 45,000 rows in a second round of 96
+// blocks 98 and 87, 60,000 rows 105 and 119).
 static bool ffn_res_fwd(const FfnShape& d) {
     if (!ffn_res_can(d)) return false;
     const int c = d.ci > d.co ? d.ci : d.co;
     return c > 128 ? ffn_fills(d.n) : ceil_div(d.n, 128) >= (c > 64 ? 100 : 40);
 }
 // Backward: once H, dG and dU outgrow the 256 MB of the last-level cache, where the tiles' traffic costs more than their better
-// spread over the device saves (forward and backward of 128 channels, 512 hidden: 60,000 rows 155 us, tiles 148; 90,000 rows
-// 217 and 224; 200,000 rows 471 and 519), and not for 64 channels or less (200,000 rows of 64: 221 and 215).
+// spread over the device saves (128 channels, 512 hidden: 60,000 rows 159 us, tiles 152; 90,000 rows 222 and 232; 200,000
+// rows 477 and 520; 256 channels, 1,024 hidden: 30,000 rows 192 and 199, 90,000 rows 521 and 584), and not for 64 channels or
+// less (forward and backward of 200,000 rows of 64: 221 and 215, with a kernel for them that is not here any more).
 static bool ffn_res_bwd(const FfnShape& d) {
     return ffn_res_can(d) && (d.ci > 64 || d.co > 64) && d.n * d.fp * 6 >= (int64_t)256 << 20;
 }
@@ -669,10 +670,10 @@ static bool ffn_launches(int dtype, const FfnShape& d, bool bwd) {
 // float32: tiles of 64 outputs instead of 128 in a direction where they leave less of the last one empty.
 static bool ffn_narrow(int64_t rows) { return ceil_div(rows, 64) % 2 == 1 && rows < 512; }
 
-// Row chunks of the weights' gradients: as many as fill the device once with two blocks a compute unit (a few blocks more
-// would take a second round: 1,032 blocks 605 us, 504 blocks 525 us), of at least 512 rows, or 128 up to 32 chunks: few rows
+// Row chunks of the weights' gradients: as many as fill the device once with two blocks a compute unit (twice as many blocks:
+// backward pass of 300,000 rows, 256 channels, 1,024 hidden bf16 1,633 us, 1,589; 30,000 rows 243 and 203), of at least 512 rows, or 128 up to 32 chunks: few rows
 // leave the device to few blocks, whose length is what counts, many rows pay for each chunk's sums (backward pass, 64 channels,
-// 256 hidden float32: 1,000 rows 35 us in chunks of 128 and 52 of 512; bfloat16: 30,000 rows 50 and 45 us).
+// 256 hidden float32: 1,000 rows 35 us in chunks of 128 and 52 of 512; bfloat16: 30,000 rows 51 and 45 us).
 static int64_t ffn_chunks(int64_t n, int64_t tiles) {
     int64_t most = ceil_div(n, 128);
     if (most > 32) most = ceil_div(n, 512) > 32 ? ceil_div(n, 512) : 32;

@@ -11,16 +11,18 @@
 // fragment is one 16-byte read per lane at a constant offset, which is started well before the product that needs it:
 // every stage is an array of its own, so that the compiler can tell the copies into one from the reads of another.
 //
-// What bounds it: the matrix cores and the activation's vector instructions, about as much time each.  The two waves of a
-// SIMD pass the same barriers, so they would do the same at the same time; therefore the products of a chunk are
-// interleaved with the activation of the chunk before it.
+// What bounds it: LDS reads, the matrix cores and the activation's vector instructions together (cycles below; the activation
+// about 2,500), which overlap little.  The two waves of a SIMD pass the same barriers, so they would do the same at the same
+// time; therefore the products of a chunk are interleaved with the activation of the chunk before it.
 //
 // Wave (m, n) of 4 x 2: rows 32 m .., hidden columns 32 n .. of a chunk; in the output projection output columns
 // 16 TT n .. .  The MFMA takes the weights first: lane (i, h) of a 32 x 32 tile gets row i and columns 8 g + 4 h + e in
 // register 4 g + e.
 //
 // 300,000 rows, 256 channels, 1,024 hidden: with the weights read as they lie by transpose reads in blocks of assembly that
-// wait for themselves, 705 us forward and 835 us for k_ffn_mid_res; packed, without the interleaving, 597 and 840 us.
+// wait for themselves, 705 us forward and 835 us for k_ffn_mid_res; packed, without the interleaving, 597 and 840 us; as they are
+// 568 and 722.  A chunk of 64 hidden columns costs a compute unit 3,072 cycles of MFMA and, in 1 KiB fragments at 128 bytes a
+// cycle, 3,300 (forward) and 4,096 cycles of LDS reads beside the activation, and takes about 8,500 and 10,800.
 #include "ffn_res.h"
 
 #include "ffn_act.h"

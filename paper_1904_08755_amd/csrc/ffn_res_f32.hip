@@ -8,7 +8,7 @@
 // second pass over dG and dU, and a row is read once instead of once per 64 hidden columns.
 //
 // Bound: the matrix cores (float32 at a sixteenth of the bfloat16 rate; the 32 x 32 x 2 instruction reaches 156 TFLOP/s on this
-// device, the 16 x 16 x 4 one of the tiles 136).  120,011 rows, 64 channels, 256 hidden: forward 126 us (tiles 160), backward
+// device, the 16 x 16 x 4 one of the tiles 136).  120,011 rows, 64 channels, 256 hidden: forward 125 us (tiles 160), backward
 // without the weights' gradients 235 us (tiles 300); without its stores 197, without the activation the same.  3,751 wave
 // tiles over 1,024 SIMDs are four rounds of which 3.66 are full.
 #include "ffn_res.h"

@@ -17,8 +17,9 @@
 // in the registers of LPR lanes (NV pieces of 16 bytes a lane), so it is read once; a wave holds
 // 64 / LPR rows, reduces each with log2(LPR) lane exchanges and needs no LDS, and the lanes keep
 // their columns' gamma, beta and (backward) column sums in registers over all rows they visit.
-// Measured: 300,000 rows of 256 bfloat16 columns forward 55 us (5.6 TB/s), backward 92 us and 5 us for the sums (5.0 TB/s);
-// 20,011 rows of 1,027 (rows at odd addresses, a third of the lanes idle in the last piece) 20 and 36 us (4.2 and 3.5 TB/s).
+// Measured: 300,000 rows of 256 bfloat16 columns forward 56 us (5.5 TB/s), backward 91 us and 4 us for the sums (5.0 TB/s);
+// 20,011 rows of 1,027 (rows at odd addresses, a third of the lanes idle in the last piece) 21 and 36 us (3.8 and 3.5 TB/s);
+// 20,000 rows of 4,096 bfloat16 columns, element by element, forward 212 us, backward 236 us (1.5 and 2.1 TB/s).
 // Rows of more than kLnRegCols columns take a block each and are read again for each sum (from the L2); with the sums over
 // rows the backward pass is a block a row for the rows' means, and then a thread a column for dX and the sums.
 #include "row_vec.h"
@@ -31,8 +32,8 @@ constexpr int kLnMaxCols = 1 << 30;
 constexpr int64_t kLnFwdBlocks = 2048;  // blocks that walk over the rows (8 a CU)
 constexpr int64_t kLnChunks = 1024;     // row chunks (blocks) of the backward pass: as many partial column sums
 // Wide rows with many elements a lane take half as many of either: fewer blocks fit a CU, and the columns' arrays and sums that
-// a block starts and ends with are long (bfloat16 backward, 20,000 rows of 1,024 columns 27 us, 29 with all of them; 205,400
-// rows of 100 columns 70 and 45; float32, 79,922 rows of 257 columns in 12 elements a lane 51 and 44).
+// a block starts and ends with are long (bfloat16 backward, 20,000 rows of 1,024 columns 28 us, 30 with all of them; 205,400
+// rows of 100 columns 44 and 31; float32, 79,922 rows of 257 columns in 12 elements a lane 53 and 45).
 static int64_t ln_most(int c, int per_lane, int64_t most) { return c > 256 && per_lane >= 16 ? most / 2 : most; }
 constexpr int kLnSumCh = 16, kLnSumLanes = 64;
 constexpr int64_t kLnSumBlocks = 65536;   // (a launch takes fewer than 2^32 threads: 2^22 blocks of these)
