@@ -15,10 +15,10 @@
 // bit-reproducible.
 //
 // bfloat16: G, U, dH and all sums stay in float32; H (but for a few rows), dG and dU are rounded to bfloat16 once, as the
-// matrix cores take them, and the results once as they are stored.  Its tiles copy operands straight into LDS (ffn_bf16.h), which takes rows of whole
-// 16-byte pieces at 16-byte addresses: operands that are not are copied into the workspace first, their rows padded with zeros
-// (k_ffn_pad; the weights and at most two passes over rows, against kernels that would load element by element).  float32
-// tiles (ffn_f32.h) take any address.
+// matrix cores take them, and the results once as they are stored.  Its tiles copy operands straight into LDS (ffn_bf16.h),
+// which takes rows of whole 16-byte pieces at 16-byte addresses: operands that are not are copied into the workspace first,
+// their rows padded with zeros (k_ffn_pad; the weights and at most two passes over rows, against kernels that would load
+// element by element).  float32 tiles (ffn_f32.h) take any address.
 #include "ffn_act.h"
 #include "ffn_bf16.h"
 #include "ffn_f32.h"
@@ -319,10 +319,11 @@ k_ffn_gemm_bf16(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n,
     store_tile(acc, r0 + 16 * MT * (wave / WN), c0 + 64 * (wave % WN), n, co, Out, co);
 }
 
-// Out (n x co, at most 256) = A1 B1 + A2 B2 for KC operands in tiles of 256 x 256: eight waves of 64 x 128 (v_mfma_f32_32x32x16_bf16), a
-// ring of four stages of 32 reduction elements, each an array of its own: the operands are plain reads, which the compiler
-// starts ahead of the products without waiting for copies into other stages.  Bound: about as much time in the copies as in
-// the products (300,000 rows, 256 columns, 2 x 1,024 elements: 385 us; without the copies 288, without the products 368).
+// Out (n x co, at most 256) = A1 B1 + A2 B2 for KC operands in tiles of 256 x 256: eight waves of 64 x 128
+// (v_mfma_f32_32x32x16_bf16), a ring of four stages of 32 reduction elements, each an array of its own: the operands are
+// plain reads, which the compiler starts ahead of the products without waiting for copies into other stages.  Bound: about as
+// much time in the copies as in the products (300,000 rows, 256 columns, 2 x 1,024 elements: 385 us; without the copies 288,
+// without the products 368).
 __global__ void __launch_bounds__(512, 1)
 k_ffn_gemm_kc(RowMat<const uint16_t> A1, RowMat<const uint16_t> A2, int64_t n, int64_t k, const uint16_t* __restrict__ B1,
               const uint16_t* __restrict__ B2, int64_t ldb, int co, uint16_t* __restrict__ Out) {
@@ -621,11 +622,11 @@ static bool ffn_fills(int64_t n) {
 static bool ffn_res_can(const FfnShape& d) { return d.ci <= kResMax && d.co <= kResMax; }
 
 // ... and do.  Forward, up to 64 channels: from 40 tiles of 128 rows on (64 channels, 1,024 hidden: 4,000 rows 23.0 us, tiles
-// 21.6; 6,000 rows 23.0 and 23.3; 12,000 rows 23.0 and 27.8; 256 hidden: 4,000 rows 10.8 and 10.9, 12,000 rows 10.9 and 12.0; 32
-// channels alike, 8 and 16 no difference).  Up to 128 channels: from 100 tiles on (128 channels, 512 hidden: 10,000 rows 19.0
-// and 17.8, 14,000 rows 19.2 and 20.6; 96 channels: 10,000 rows 15.0 and 14.4, 14,000 rows 15.2 and 16.0).  Wider ones take a block a
-// compute unit: where they fill their rounds (256 channels: 30,000 rows 57 and 62 us, 45,000 rows in a second round of 96
-// blocks 98 and 87, 60,000 rows 105 and 119).
+// 21.6; 6,000 rows 23.0 and 23.3; 12,000 rows 23.0 and 27.8; 256 hidden: 4,000 rows 10.8 and 10.9, 12,000 rows 10.9 and 12.0;
+// 32 channels alike, 8 and 16 no difference).  Up to 128 channels: from 100 tiles on (128 channels, 512 hidden: 10,000 rows
+// 19.0 and 17.8, 14,000 rows 19.2 and 20.6; 96 channels: 10,000 rows 15.0 and 14.4, 14,000 rows 15.2 and 16.0).  Wider ones
+// take a block a compute unit: where they fill their rounds (256 channels: 30,000 rows 57 and 62 us, 45,000 rows in a second
+// round of 96 blocks 98 and 87, 60,000 rows 105 and 119).
 static bool ffn_res_fwd(const FfnShape& d) {
     if (!ffn_res_can(d)) return false;
     const int c = d.ci > d.co ? d.ci : d.co;
@@ -640,11 +641,11 @@ static bool ffn_res_bwd(const FfnShape& d) {
 }
 
 // float32: where the blocks fill their rounds (64 channels, 256 hidden, forward 16,000 rows 31 us, tiles 26; 32,000 rows 32
-// and 41; 60,000 rows 55 and 70; backward 89 and 71, 110 and 116, 172 and 187, but 45,000 rows 162 and 150).  Forward of up to 32
-// channels, of which a compute unit takes several blocks: up to 128 hidden columns always (300 to 8,000 rows 10.5 to 10.8
-// us, tiles 10.8 to 11.2; 45,000 rows 18 and 25), more of them, which a block walks over one chunk after the other, from 150 tiles
-// on (256 hidden: 1,000 rows 18.6 us, tiles 13.1, 16,000 rows 18.9 and 20.3, 24,000 rows 19.5 and 27.8; 1,024 hidden: 65 and 33,
-// 68 and 59, 67 and 86; 45,000 rows 111 and 136).
+// and 41; 60,000 rows 55 and 70; backward 89 and 71, 110 and 116, 172 and 187, but 45,000 rows 162 and 150).  Forward of up
+// to 32 channels, of which a compute unit takes several blocks: up to 128 hidden columns always (300 to 8,000 rows 10.5 to
+// 10.8 us, tiles 10.8 to 11.2; 45,000 rows 18 and 25), more of them, which a block walks over one chunk after the other, from
+// 150 tiles on (256 hidden: 1,000 rows 18.6 us, tiles 13.1, 16,000 rows 18.9 and 20.3, 24,000 rows 19.5 and 27.8; 1,024
+// hidden: 65 and 33, 68 and 59, 67 and 86; 45,000 rows 111 and 136).
 static bool ffn_res_f32(const FfnShape& d, bool bwd) {
     if (d.ci > kResMaxF32 || d.co > kResMaxF32) return false;
     return ffn_fills(d.n) || (!bwd && d.ci <= 32 && d.co <= 32 && (d.f <= 128 || ceil_div(d.n, 128) >= 150));
@@ -671,9 +672,10 @@ static bool ffn_launches(int dtype, const FfnShape& d, bool bwd) {
 static bool ffn_narrow(int64_t rows) { return ceil_div(rows, 64) % 2 == 1 && rows < 512; }
 
 // Row chunks of the weights' gradients: as many as fill the device once with two blocks a compute unit (twice as many blocks:
-// backward pass of 300,000 rows, 256 channels, 1,024 hidden bf16 1,633 us, 1,589; 30,000 rows 243 and 203), of at least 512 rows, or 128 up to 32 chunks: few rows
-// leave the device to few blocks, whose length is what counts, many rows pay for each chunk's sums (backward pass, 64 channels,
-// 256 hidden float32: 1,000 rows 35 us in chunks of 128 and 52 of 512; bfloat16: 30,000 rows 51 and 45 us).
+// backward pass of 300,000 rows, 256 channels, 1,024 hidden bf16 1,633 us, 1,589; 30,000 rows 243 and 203), of at least 512
+// rows, or 128 up to 32 chunks: few rows leave the device to few blocks, whose length is what counts, many rows pay for each
+// chunk's sums (backward pass, 64 channels, 256 hidden float32: 1,000 rows 35 us in chunks of 128 and 52 of 512; bfloat16:
+// 30,000 rows 51 and 45 us).
 static int64_t ffn_chunks(int64_t n, int64_t tiles) {
     int64_t most = ceil_div(n, 128);
     if (most > 32) most = ceil_div(n, 512) > 32 ? ceil_div(n, 512) : 32;
@@ -775,9 +777,9 @@ static void ffn_fwd(const FfnShape& d, const FfnLayout& L, const float* X, const
     });
 }
 
-static void ffn_bwd_rows(const FfnShape& d, const FfnLayout& L, const float* X, const float* Wg, const float* Wu, const float* Wd,
-                         const float* dY, int act, float* dX, RowMat<float> H, RowMat<float> dG, RowMat<float> dU,
-                         hipStream_t s) {
+static void ffn_bwd_rows(const FfnShape& d, const FfnLayout& L, const float* X, const float* Wg, const float* Wu,
+                         const float* Wd, const float* dY, int act, float* dX, RowMat<float> H, RowMat<float> dG,
+                         RowMat<float> dU, hipStream_t s) {
     if (L.res) return res_bwd(X, dY, d.n, d.ci, Wg, Wu, d.f, Wd, d.co, act, (int)d.fp, H, dG, dU, dX, s);
     const int nf = (int)ceil_div(d.f, 64);
     const bool sho = ffn_short(d.n, 128, nf);

@@ -15,10 +15,10 @@ __device__ __forceinline__ void ffn_sigmoid(float x, float& p, float& q) {
     if (D) q = fminf(e * p, 1.f);   // (e = infinity, p = 0: the minimum of a NaN and 1 is 1)
 }
 
-// P(g) of the normal distribution function from e = exp(-g^2 / 2).  Up to |g| = 1 it is 1/2 + g S(g^2), beyond it
-// q = P(-|g|) = e t T(t) with t = 1 / (1 + 0.39 |g|); either polynomial is the least-error fit of its degree, S within 7.4e-9
-// absolutely and T within 1.0e-7 of its value out to where q leaves float32's range.  SHORT: one such fit for all g, within
-// 7.9e-7 of q, for values that are rounded to bfloat16 (300,000 rows, 256 channels, 1,024 hidden forward 583 us, 611 with both).
+// P(g) of the normal distribution function from e = exp(-g^2 / 2).  Up to |g| = 1 it is 1/2 + g S(g^2), beyond it q = P(-|g|)
+// = e t T(t) with t = 1 / (1 + 0.39 |g|); either polynomial is the least-error fit of its degree, S within 7.4e-9 absolutely
+// and T within 1.0e-7 of its value out to where q leaves float32's range.  SHORT: one such fit for all g, within 7.9e-7 of q,
+// for values that are rounded to bfloat16 (300,000 rows, 256 channels, 1,024 hidden forward 583 us, 611 with both).
 template <bool SHORT>
 __device__ __forceinline__ float ffn_normal(float g, float e) {
     const float z = fabsf(g);

@@ -20,9 +20,9 @@
 // register 4 g + e.
 //
 // 300,000 rows, 256 channels, 1,024 hidden: with the weights read as they lie by transpose reads in blocks of assembly that
-// wait for themselves, 705 us forward and 835 us for k_ffn_mid_res; packed, without the interleaving, 597 and 840 us; as they are
-// 568 and 722.  A chunk of 64 hidden columns costs a compute unit 3,072 cycles of MFMA and, in 1 KiB fragments at 128 bytes a
-// cycle, 3,300 (forward) and 4,096 cycles of LDS reads beside the activation, and takes about 8,500 and 10,800.
+// wait for themselves, 705 us forward and 835 us for k_ffn_mid_res; packed, without the interleaving, 597 and 840 us; as they
+// are 568 and 722.  A chunk of 64 hidden columns costs a compute unit about 3,100 cycles of MFMA and, in 1 KiB fragments at
+// 128 bytes a cycle, 3,300 (forward) and 4,096 cycles of LDS reads beside the activation, and takes about 8,500 and 10,800.
 #include "ffn_res.h"
 
 #include "ffn_act.h"

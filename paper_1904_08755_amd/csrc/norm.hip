@@ -7,11 +7,12 @@
 // bit-reproducible.
 //
 // The mean is taken in two steps: m1 = x[0] + mean(x - x[0]) rounded to float32, then, with e = x - m1, its rest m2 =
-// mean(e), a few roundings of m1's size.  x - m is e - m2 and v is mean(e^2) - m2^2, both sums in one round of
-// exchanges.  (The difference loses no digits: m2 is at most about half a step of float32 at m1, and rows that are not
-// constant have a deviation of that size at least.)  So neither an offset that a row's values share nor a first value far
-// larger than the others costs digits.  The backward pass gets m1 + m2 rounded to float32, and where a row's values share an
-// offset that rounding is as large as their deviations: it takes x - mean, and out of that the rest's mean, again.
+// mean(e).  x - m is e - m2 and v is mean(e^2) - m2^2, both sums in one round of exchanges.  So neither an offset that a row's
+// values share nor a first value far larger than the others costs digits.  (Nor does the difference: m2 is half a step of
+// float32 at m1, which the deviation of a row that is not constant reaches, and the sum's roundings of x - x[0], a
+// millionth of it, where the deviation is |x - x[0]| / sqrt(c) or more.)  The backward pass gets m1 + m2 rounded to float32,
+// and where a row's values share an offset that rounding is as large as their deviations: it takes x - mean, and out of that
+// the rest's mean, again.
 //
 // Bound: HBM (a read and a write of n x c forward, two reads and a write backward).  A row stays
 // in the registers of LPR lanes (NV pieces of 16 bytes a lane), so it is read once; a wave holds
@@ -449,7 +450,8 @@ static int64_t ln_bwd(const void* X_, const void* dY_, int64_t n, int c, const f
     T* dX = reinterpret_cast<T*>(dX_);
     int64_t chunks = 0;
     if (c > kLnRegCols) {
-        // of 64 rows, or of fewer, down to 8, while there are under 1,024 blocks (300 rows of 8,192 bfloat16 columns: 23 us, 29)
+        // of 64 rows, or of fewer, down to 8, while there are under 1,024 blocks (300 rows of 8,192 bfloat16 columns: 23 us,
+        // 29)
         const unsigned cb = (unsigned)((c + kLnThreads - 1) / kLnThreads);
         const int64_t most = ln_row_blocks(n, 8, 1024 / cb + 1);
         chunks = ln_row_blocks(n, 64, kLnChunks);
