@@ -567,10 +567,11 @@ int gsc_global_pool_bwd(int32_t mode, const float* dY, int32_t n_batch, int32_t 
  * 0); eps >= 0.  mean, rstd (n float32 values, each nullable) receive m and r,
  * which the backward pass takes.  n = 0 does nothing.  A row with a NaN or an
  * infinity becomes NaN, and no other row does.  Deviations x - m are off by a
- * few float32 roundings of their own sizes and of their mean size, whatever
- * offset the row's values share and wherever its largest one stands; the sum of
- * the squares of x - m has to lie in float32's range (values to about 1e19 /
- * sqrt(c)).  Asynchronous.  Errors: EINVAL (c from 1 to 2^30), EHIP. */
+ * few float32 roundings of their own sizes and at most max(32, c / 256) + 12 of
+ * their mean size, whatever offset the row's values share and wherever its
+ * largest one stands; the sum of the squares of x - m has to lie in float32's
+ * range (values to about 1e19 / sqrt(c)).  Asynchronous.  Errors: EINVAL (c from
+ * 1 to 2^30), EHIP. */
 int gsc_layer_norm_fwd(int32_t dtype, const void* X, int64_t n, int32_t c, const float* gamma, const float* beta,
                        float eps, void* Y, float* mean, float* rstd, void* stream);
 
